@@ -116,6 +116,16 @@ cudaError_t opt_in_smem(Kernel kernel, int bytes, std::atomic<unsigned long long
 }
 
 // page bookkeeping (hs2_pages.cu)
+__host__ __device__ __forceinline__ int pages_of(int len, int ps) { return (int)(((int64_t)len + ps - 1) / ps); }
+// The table entries of a sequence of `len` tokens that go when it keeps the first `keep` of them: x .. y - 1, and none at x >= y.
+// A keep of any size names no entry behind those of the sequence, so that a thread's index added to x stays in int32.
+__host__ __device__ __forceinline__ int2 released_entries(int len, int keep, int ps, int max_pages)
+{
+    const int held = len < 0 ? 0 : len, kept = keep < 0 ? 0 : keep;
+    const int have = pages_of(held, ps), end = have < max_pages ? have : max_pages;
+    return make_int2(pages_of(kept < held ? kept : held, ps), end);
+}
+
 struct PageRegions {
     hs2_page_region r[HS2_MAX_PAGE_REGIONS];
     int n;

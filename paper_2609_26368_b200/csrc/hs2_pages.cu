@@ -51,8 +51,6 @@ size_t layout(const hs2_page_pool &pool, int n, void *ws, PagesWs *out)
     return at;
 }
 
-__device__ __forceinline__ int pages_of(int len, int ps) { return (int)(((int64_t)len + ps - 1) / ps); }
-
 // exclusive prefix of `v` over the CTA; `total` the sum
 template <typename T>
 __device__ __forceinline__ T cta_scan(T v, T &total, T *scratch /* [32] */)
@@ -453,9 +451,9 @@ k_pages_free(const hs2_page_pool pool, const int32_t *__restrict__ seqs, const i
     if (s < 0 || s >= pool.max_seqs) return;
     const int kept = keep ? max(0, keep[i]) : 0;
     const int len = *reinterpret_cast<volatile int32_t *>(pool.lens + s);
-    const int have = min(pages_of(max(0, len), pool.page_size), pool.max_pages);
+    const int2 gone = released_entries(len, kept, pool.page_size, pool.max_pages);
     int32_t *row = pool.page_table + (int64_t)s * pool.max_pages;
-    for (int c = pages_of(kept, pool.page_size) + threadIdx.x; c < have; c += 128) {
+    for (int64_t c = (int64_t)gone.x + threadIdx.x; c < gone.y; c += 128) {
         const int p = atomicExch(row + c, -1);
         if (p >= 0 && p < pool.n_pages) atomicSub(pool.ref_counts + p, 1);
     }

@@ -1,0 +1,53 @@
+"""CPU checks of host code and index arithmetic that the sliding-window, paged-decode and page calls share with their kernels."""
+import os
+import random
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2609_26368_b200 import build as build_module
+
+INT_MAX = 2 ** 31 - 1
+
+
+def run_host_code(tmp_path, body, lines):
+    """Compiles `body`, a main() that reads numbers and prints answers, with the kernels' own header for the host, and runs it."""
+    if shutil.which("nvcc") is None:
+        pytest.skip("no nvcc")
+    src, exe = tmp_path / "host.cu", tmp_path / "host"
+    src.write_text('#include <stdio.h>\n#include "hs2_paged.cuh"\n' + body)
+    include = os.path.join(os.path.dirname(os.path.dirname(build_module.CSRC)), "include")
+    subprocess.check_call(["nvcc", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I" + include, "-I" + build_module.CSRC,
+                           str(src), "-o", str(exe)])
+    out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, x)) for x in lines), text=True, capture_output=True, check=True)
+    return [tuple(map(int, line.split())) for line in out.stdout.splitlines()]
+
+
+def test_released_entries_stay_in_the_row_for_any_keep(tmp_path):
+    """hs2_pages_free: with one token per page a keep near INT_MAX is as many pages, and a thread's index on top of that wraps."""
+    rng = random.Random(1)
+    cases = []
+    for _ in range(400):
+        ps = rng.choice([1, 1, 2, 16, 1000])
+        max_pages = rng.choice([1, 30, 4096, INT_MAX // ps])
+        most = max_pages * ps
+        length = rng.choice([-5, 0, 1, most // 2, most, rng.randrange(most + 1)])
+        keep = rng.choice([-2 ** 31, -1, 0, 1, length, length + 1 if length < INT_MAX else length, INT_MAX - 126, INT_MAX,
+                           rng.randrange(2 ** 31)])
+        cases.append((length, keep, ps, max_pages))
+    got = run_host_code(tmp_path, """int main()
+{
+    int len, keep, ps, max_pages;
+    while (scanf("%d %d %d %d", &len, &keep, &ps, &max_pages) == 4) {
+        const int2 r = hs2::released_entries(len, keep, ps, max_pages);
+        printf("%d %d\\n", r.x, r.y);
+    }
+}
+""", cases)
+    assert len(got) == len(cases)
+    for (length, keep, ps, max_pages), (first, end) in zip(cases, got):
+        held, kept = max(0, length), max(0, keep)
+        plain = range(-(-kept // ps), min(-(-held // ps), max_pages))   # without a limit on the numbers
+        assert 0 <= end <= max_pages and 0 <= first <= max(end, -(-held // ps))
+        assert max(0, end - first) == len(plain) and (not plain or first == plain[0])
