@@ -63,8 +63,10 @@ struct Cfg {
 };
 
 enum Bar {
-    Q_FULL = 0, Q_FREE = 2, BUF_FREE = 4, S_FULL = 6, P_FULL = 10, PV_DONE = 14, O_FULL = 18, O_FREE, STAT_FULL, STAT_FREE, G_FULL,
-    C_FULL, C_FREE = C_FULL + 4, R_FULL = C_FREE + 4, R_FREE = R_FULL + 6, N_BARS = R_FREE + 6
+    Q_FULL = 0, Q_FREE = 2, BUF_FREE = 4, S_FULL = 6, P_FULL = 10, PV_DONE = 14, O_FULL = 18, O_FREE, STAT_FULL, STAT_FREE,
+    G_FULL = 22,                   // of the gate in either Q buffer: with one for both, the gate of the next row tile, which needs only
+                                   // its own Q K^T, could land before the epilogue has looked for this one's
+    C_FULL = 24, C_FREE = C_FULL + 4, R_FULL = C_FREE + 4, R_FREE = R_FULL + 6, N_BARS = R_FREE + 6
 };
 static_assert(N_BARS * 8 + 8 <= 384, "barriers fit");
 
@@ -380,9 +382,9 @@ k_window_tc5(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                     ok = ok && load(j < t.n_a ? &tmF : &tmV, t, j);
                 }
                 if (ok && a.has_gate && (ok = wait(bar(Q_FREE + (k & 1)), (k >> 1) & 1, abort_flag))) {   // into Q's place
-                    mbar_expect_tx(bar(G_FULL), NQ * a.rows * 128);
+                    mbar_expect_tx(bar(G_FULL + (k & 1)), NQ * a.rows * 128);
 #pragma unroll
-                    for (int sl = 0; sl < NQ; ++sl) tma_load_4d(buffer(k) + sl * BM * 128, &tmG, bar(G_FULL), 64 * sl, t.h0, t.i0, t.b);
+                    for (int sl = 0; sl < NQ; ++sl) tma_load_4d(buffer(k) + sl * BM * 128, &tmG, bar(G_FULL + (k & 1)), 64 * sl, t.h0, t.i0, t.b);
                     ++n_g;
                 }
                 if (ok) at = next_item(k, true);
@@ -392,7 +394,7 @@ k_window_tc5(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                 for (uint32_t u = r > NR ? r - NR : 0; u < r; ++u) land(bar(R_FULL + u % NR), (u / NR) & 1);
                 for (uint32_t u = k > 4 ? k - 4 : 0; u < k; ++u) land(bar(C_FULL + (u & 3)), (u >> 2) & 1);
                 for (uint32_t u = k > 2 ? k - 2 : 0; u < k; ++u) land(bar(Q_FULL + (u & 1)), (u >> 1) & 1);
-                if (n_g > 0) land(bar(G_FULL), (n_g - 1) & 1);
+                for (uint32_t u = n_g > 2 ? n_g - 2 : 0; u < n_g; ++u) land(bar(G_FULL + (u & 1)), (u >> 1) & 1);
             }
         }
     } else if (warp == F::kMmaWarp) {
@@ -498,7 +500,7 @@ k_window_tc5(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         // The output of row tile k; false: somebody gave up, all leave.
         auto epilogue = [&](const Item &t, float inv, int c0, int c1) -> bool {
             if (ok) ok = __all_sync(0xffffffffu, wait(bar(O_FULL), k & 1, abort_flag));
-            if (ok && a.has_gate) ok = __all_sync(0xffffffffu, wait(bar(G_FULL), k & 1, abort_flag));
+            if (ok && a.has_gate) ok = __all_sync(0xffffffffu, wait(bar(G_FULL + (k & 1)), (k >> 1) & 1, abort_flag));
             if (!group_all(1, F::kEpiWarps * 32, ok)) return ok = false;
             tc_fence_after();
             finish_row<D>(a, t, lanes + F::kColO, smem + F::kOffQ + (k & 1) * F::kQ, row, t.i0 + q_in, t.h0 + h_in, inv, c0, c1);

@@ -31,3 +31,66 @@ def test_pages_free_keeps_everything_for_a_keep_of_any_size(ps):
         plain.free(seqs, keep)
         assert pool.ref_counts.tolist() == plain.refs and pool.lens.tolist() == plain.lens
         assert pool.page_table.tolist() == plain.matrix()
+
+
+# ---------------------------------------------------------------- sliding window: many row tiles per CTA
+MANY = [
+    # Hq, Hkv, D, w, first, B, Lq, Lk: with one, two, three and more key tiles per row tile, and thousands of row tiles
+    (16, 2, 64, 20, 0, 2, 9001, 9100),
+    (16, 2, 64, 49, 3, 2, 9001, 9100),
+    (16, 2, 64, 130, 70, 2, 5000, 5007),
+    (32, 4, 128, 20, 0, 2, 5000, 5100),
+    (32, 4, 128, 49, 4, 2, 5000, 5100),
+    (32, 4, 128, 100, 0, 2, 5000, 5000),
+    (24, 8, 128, 300, 5, 2, 4001, 4100),
+    (64, 1, 256, 20, 0, 2, 3001, 3100),
+    (64, 1, 256, 63, 0, 2, 3001, 3100),
+    (64, 1, 256, 64, 2, 2, 3001, 3100),
+    (64, 1, 256, 128, 0, 2, 3001, 3100),
+    (5, 1, 256, 250, 1, 1, 12000, 12001),
+]
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gate"])
+@pytest.mark.parametrize("case", MANY, ids=str)
+def test_window_of_many_row_tiles(case, gated):
+    """Each CTA works through many row tiles, whose loads, products and outputs overlap.  All rows are compared with the fp32
+    kernel, which has one row tile per CTA, and sampled ones with the 64-bit form.
+
+    Bounds as in plain_ops; the weights' sum A = sum_j w_j |v_j| comes from the fp32 kernel on |v|.  Both sides have the error of a
+    logit, at most (D + 4) 2^-24 scale |q| |k|, so a weight may differ by 4 of them relative to itself."""
+    Hq, Hkv, D, w, nf, B, Lq, Lk = case
+    g = torch.Generator().manual_seed(sum(case))
+    q, k, v = rand(g, B, Lq, Hq, D, scale=1.5), rand(g, B, Lk, Hkv, D), rand(g, B, Lk, Hkv, D)
+    sink = torch.randn(Hq, generator=g)
+    gate = rand(g, B, Lq, Hq, D, scale=2.0) if gated else None
+    lens, starts = [Lk, max(1, Lk - 700)][:B], [Lk - Lq, 11][:B]
+    kd, vd = k.cuda(), v.cuda()
+    for b in range(B):   # what lies behind a cache's end is never part of an answer
+        kd[b, lens[b]:], vd[b, lens[b]:] = NAN, NAN
+    prob = hs2.Problem.from_tensors(q, k, 0, w, q_start=i32(starts), kv_lens=i32(lens))
+    qd, sd, gd = q.cuda(), sink.cuda(), None if gate is None else gate.cuda()
+    out, lse = hs2.hs2_window_attn(prob, qd, kd, vd, nf, sink=sd, gate=gd, want_lse=True)
+    assert hs2.hs2_device_error_flags() == 0
+    p32 = hs2.Problem.from_tensors(qd.float(), k, 0, w, q_start=i32(starts), kv_lens=i32(lens))
+    call32 = lambda x: hs2.hs2_window_attn(p32, qd.float(), kd.float(), x.float(), nf, sink=sd, gate=None if gd is None else gd.float(), want_lse=True)  # noqa: E731
+    (o32, l32), (A32, _) = call32(vd), call32(vd.abs())
+    logit = (D + 4) * 2.0 ** -24 * D ** -0.5 * float(q.float().norm(dim=-1).max() * k.float().norm(dim=-1).max()) + 2.0 ** -18
+    tol = 2.0 ** -8 * o32.abs() + A32 * (2.0 ** -8 + 4 * logit) + 1e-30
+    assert torch.isfinite(out).all()
+    off = (out.float() - o32).abs() > tol
+    assert not off.any(), "%d outputs off, worst %.3g of its bound" % (int(off.sum()), float(((out.float() - o32).abs() / tol).max()))
+    assert torch.equal(lse.isinf(), l32.isinf())
+    some = ~l32.isinf()
+    assert ((lse - l32)[some].abs() <= 2 * logit + 2.0 ** -20 * l32[some].abs()).all()
+    again, _ = hs2.hs2_window_attn(prob, qd, kd, vd, nf, sink=sd, gate=gd)
+    assert torch.equal(out, again)
+    # sampled rows
+    for n in range(24):
+        b, i = n % B, int(torch.randint(Lq, (), generator=g)) if n > 4 else [0, Lq - 1, Lq // 2, 1, 127][n]
+        pos = starts[b] + i
+        keys = [j for j in range(min(pos + 1, lens[b])) if j > pos - w or j < nf]
+        rows = [x[b, keys].transpose(0, 1).repeat_interleave(Hq // Hkv, 0) for x in (k, v)]
+        r = plain_ops.attend(q[b, i], *rows, torch.ones(Hq, len(keys), dtype=torch.bool), D ** -0.5, sink, None if gate is None else gate[b, i])
+        ref = r[0][None, None], r[1][None, :, None], r[2][None, None], r[3][None, :, None]
+        plain_ops.check(out[b, i][None, None], lse[b, :, i][None, :, None], ref, D, "row %d of %d" % (i, b))
