@@ -39,6 +39,7 @@ using namespace tc5;
 
 constexpr int BM = 128, BN = 64;
 constexpr float kRescale = 8.f;   // log2 units
+constexpr float kPairedGate = -41.f;   // above it 1 + e^-x is below 2^60, and the product of two of them a normal number
 
 template <int D>
 struct Cfg {
@@ -286,13 +287,16 @@ __device__ __forceinline__ void finish_row(const WindowArgs &a, const Item &t, u
                 const uint32_t wd[4] = {gt.x, gt.y, gt.z, gt.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    // x / (1 + 2^u) and y / (1 + 2^v) with one reciprocal (the exponential unit is the busiest one here); the
-                    // exponents are capped so that the product stays finite: a factor below 2^-60 becomes 2^-60
-                    const float u = 1.f + exp2f(fminf(__uint_as_float(wd[e] << 16) * -kLog2e, 60.f));
-                    const float v = 1.f + exp2f(fminf(__uint_as_float(wd[e] & 0xffff0000u) * -kLog2e, 60.f));
-                    const float inv_uv = __fdividef(1.f, u * v);
-                    f[2 * e] *= v * inv_uv;
-                    f[2 * e + 1] *= u * inv_uv;
+                    const float x = __uint_as_float(wd[e] << 16), y = __uint_as_float(wd[e] & 0xffff0000u);
+                    if (x > kPairedGate && y > kPairedGate) {
+                        // 1 / (1 + e^-x) and 1 / (1 + e^-y) with one reciprocal: the exponential unit is the busiest one here
+                        const float u = 1.f + exp2f(x * -kLog2e), v = 1.f + exp2f(y * -kLog2e), inv_uv = __fdividef(1.f, u * v);
+                        f[2 * e] *= v * inv_uv;
+                        f[2 * e + 1] *= u * inv_uv;
+                    } else {   // NaN too
+                        f[2 * e] *= gate_of(x);
+                        f[2 * e + 1] *= gate_of(y);
+                    }
                 }
             }
             *cell = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));

@@ -94,3 +94,28 @@ def test_window_of_many_row_tiles(case, gated):
         r = plain_ops.attend(q[b, i], *rows, torch.ones(Hq, len(keys), dtype=torch.bool), D ** -0.5, sink, None if gate is None else gate[b, i])
         ref = r[0][None, None], r[1][None, :, None], r[2][None, None], r[3][None, :, None]
         plain_ops.check(out[b, i][None, None], lse[b, :, i][None, :, None], ref, D, "row %d of %d" % (i, b))
+
+
+# ---------------------------------------------------------------- gates
+@pytest.mark.parametrize("case", [(8, 2, 64, BF16, 300), (8, 1, 128, BF16, 300), (64, 1, 256, BF16, 90), (6, 2, 96, BF16, 90), (4, 2, 64, F32, 90),
+                                  (8, 2, 128, BF16, 1), (64, 1, 128, BF16, 1), (4, 2, 64, F32, 1)], ids=str)
+def test_gates_of_any_size(case):
+    """NaN logits, each of which concerns its own output alone, infinite ones, and ones so low that the factor is tiny or zero: the
+    same on every kernel."""
+    Hq, Hkv, D, dt, Lq = case
+    g = torch.Generator().manual_seed(46)
+    Lk, w = 400, 50
+    q, k, v = rand(g, 1, Lq, Hq, D, dtype=dt), rand(g, 1, Lk, Hkv, D, dtype=dt), rand(g, 1, Lk, Hkv, D, dtype=dt)
+    sink = torch.randn(Hq, generator=g)
+    gate = rand(g, 1, Lq, Hq, D, dtype=dt, scale=3.0)
+    for d, x in enumerate((NAN, 1.0, -INF, -700.0, INF, 700.0, -50.0, -60.0, -41.0, 3.0, -42.0, -80.0, 2.0, NAN, NAN, -INF)):
+        gate[0, :, Hq - 1, d] = x
+    gate[0, Lq // 2, 0] = -700.0
+    prob = hs2.Problem.from_tensors(q, k, 0, w)
+    out, lse = hs2.hs2_window_attn(prob, q.cuda(), k.cuda(), v.cuda(), 2, sink=sink.cuda(), gate=gate.cuda(), want_lse=True)
+    nan = gate.isnan().cuda()
+    assert out[nan].isnan().all()
+    assert (out[0, :, Hq - 1, [2, 3, 15]] == 0).all() and (out[0, Lq // 2, 0] == 0).all()
+    ref = plain_ops.window(q, k, v, w, 2, D ** -0.5, [Lk], [Lk - Lq], sink, gate.nan_to_num(0.0, INF, -INF))
+    out[nan] = ref[0].cuda()[nan].to(dt)
+    plain_ops.check(out, lse, ref, D, "gates")
