@@ -119,9 +119,10 @@ __device__ __forceinline__ bool wide_rows(const KV *K, int D, int64_t a, int64_t
 template <typename KV>
 __device__ __forceinline__ void fold(Row &st, float t2, unsigned mask, const KV *vrow, float vs, int D, int lane)
 {
-    const float m_new = fmaxf(st.m, warp_max(t2));
-    if (m_new == -INFINITY) return;
-    const float corr = exp2f(st.m - m_new), pj = exp2f(t2 - m_new);
+    if (mask == 0) return;
+    // (the maximum passes over NaN: of logits that are all NaN it is -inf, and they have to reach the sums all the same)
+    const float m_new = fmaxf(st.m, warp_max(t2)), base = m_new == -INFINITY ? 0.f : m_new;
+    const float corr = exp2f(st.m - base), pj = exp2f(t2 - base);
     st.l = st.l * corr + warp_sum(pj);
     st.m = m_new;
 #pragma unroll

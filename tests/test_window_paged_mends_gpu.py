@@ -119,3 +119,62 @@ def test_gates_of_any_size(case):
     ref = plain_ops.window(q, k, v, w, 2, D ** -0.5, [Lk], [Lk - Lq], sink, gate.nan_to_num(0.0, INF, -INF))
     out[nan] = ref[0].cuda()[nan].to(dt)
     plain_ops.check(out, lse, ref, D, "gates")
+
+
+# ---------------------------------------------------------------- numbers that are not finite
+def quantise(x):
+    amax = x.float().abs().amax(-1, keepdim=True).clamp(min=1e-20)
+    codes = (x.float() / (amax / 448)).to(torch.float8_e4m3fn)
+    scale = (amax / 448).squeeze(-1)
+    return codes, scale, codes.double() * scale.double()[..., None]
+
+
+# what runs the call: heads, KV heads, head dim, type, e4m3 cache, bytes that q is shifted by
+DECODES = [(8, 2, 128, F32, False, 0), (3, 1, 80, BF16, False, 0), (8, 2, 128, BF16, False, 1), (4, 2, 64, BF16, True, 0),   # FMAs
+           (8, 2, 128, BF16, False, 0), (8, 1, 128, BF16, True, 0), (20, 1, 64, BF16, False, 0),                              # mma.sync
+           (64, 1, 128, BF16, False, 0), (40, 1, 256, BF16, True, 0), (4, 1, 256, BF16, False, 0)]                            # tcgen05
+
+
+def decode_setup(g, case, lens, ps=16):
+    """A cache of the case's kind, its values, and a call of the decode with a query."""
+    Hq, Hkv, D, dt, fp8, shift = case
+    n_pages = sum(-(-n // ps) for n in lens)
+    k, v = rand(g, n_pages, ps, Hkv, D, dtype=F32 if fp8 else dt), rand(g, n_pages, ps, Hkv, D, dtype=F32 if fp8 else dt)
+    cols = max(1, max(-(-n // ps) for n in lens))
+    table, at = torch.full((len(lens), cols), -1, dtype=torch.int32), 0
+    for b, n in enumerate(lens):
+        m = -(-n // ps)
+        table[b, :m] = torch.arange(at, at + m, dtype=torch.int32)
+        at += m
+    if fp8:
+        (k8, ks, kx), (v8, vs, vx) = quantise(k), quantise(v)
+        args = [k8.view(torch.uint8).cuda(), v8.view(torch.uint8).cuda(), ks.cuda(), vs.cuda()]
+    else:
+        kx, vx, args = k, v, [k.cuda(), v.cuda()]
+
+    def call(q, **kw):
+        room = torch.zeros(q.numel() + 8, dtype=dt, device="cuda")
+        qd = room[shift:shift + q.numel()].view(q.shape)
+        qd.copy_(q)
+        prob = hs2.PagedProblem.from_tensors(qd, args[0], table.cuda(), i32(lens))
+        return (hs2.hs2_paged_attn_decode_fp8kv if fp8 else hs2.hs2_paged_attn_decode)(prob, qd, *args, want_lse=True, **kw)
+
+    return kx, vx, table, call
+
+
+@pytest.mark.parametrize("n", [1, 40, 3000])
+@pytest.mark.parametrize("case", DECODES, ids=str)
+def test_decode_of_a_query_that_is_not_a_number(case, n):
+    """One NaN in the query of one head: that head's output is NaN throughout, as the formula has it, and the other heads, and
+    the other sequences, know nothing of it."""
+    Hq, Hkv, D, dt, fp8, _ = case
+    g = torch.Generator().manual_seed(41)
+    lens = [n, 70, 0]
+    kx, vx, table, call = decode_setup(g, case, lens)
+    q = rand(g, 3, 1, Hq, D, dtype=dt)
+    ref = plain_ops.paged(q, kx, vx, table, lens, 0, 0, D ** -0.5)
+    q[0, 0, Hq - 1, 3] = NAN
+    out, lse = call(q)
+    assert out[0, 0, Hq - 1].isnan().all()
+    out[0, 0, Hq - 1], lse[0, Hq - 1] = ref[0][0, 0, Hq - 1].to(dt).cuda(), ref[1][0, Hq - 1].cuda()
+    plain_ops.check(out, lse, ref, D, "beside", p_eps=2.0 ** -8 if dt == BF16 else None)
