@@ -153,18 +153,6 @@ __device__ __forceinline__ void fold(Row &st, float t2, unsigned mask, const KV 
     }
 }
 
-// The result of a row with everything folded: the sink joins the denominator, the gate scales the output.
-template <typename T>
-__device__ __forceinline__ float denominator(float &m, float l, const float *sink, int h)
-{
-    if (sink) {
-        const float s2 = sink[h] * kLog2e, m_new = fmaxf(m, s2);
-        if (m_new != -INFINITY) l = l * exp2f(m - m_new) + exp2f(s2 - m_new);
-        m = m_new;
-    }
-    return l;
-}
-
 // ---------------------------------------------------------------- fp32 FMAs: any shape, any type
 // One CTA = one chunk of one (sequence, query head); its warps take 32 keys in turn and are joined through shared memory.
 // Bound by the latency of its loads (a lane reads its own key row), kept for the shapes the tensor-core kernels do not cover.
@@ -213,24 +201,21 @@ k_paged_generic(const PagedParams p, const T *__restrict__ Q, const KV *__restri
     }
     const bool whole = keys.n <= p.chunk;   // nothing to join: finish here
     const int64_t part = ((int64_t)b * p.Hq + h) * p.n_split + split;
-    const float den = whole ? denominator<T>(m, l, p.sink, h) : 1.f;
-    // m may have moved to the sink: the sums are relative to the maximum of the keys
-    const float m_keys = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-    const float inv = whole ? (den > 0.f ? (m_keys == -INFINITY ? 0.f : exp2f(m_keys - m)) / den : 0.f) : 1.f;
+    const RowEnd end = row_end(m, l, whole ? p.sink : nullptr, h);
     for (int d = threadIdx.x; d < p.D; d += kWarps * 32) {
         float o = 0.f;
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) o += so[i][d] * f[i];
         if (whole) {
             const int64_t at = b * p.os_b + h * p.os_h + d;
-            from_f32(O[at], o * inv * (p.gate ? gate_of(elem(static_cast<const T *>(p.gate)[at])) : 1.f));
+            from_f32(O[at], o * end.factor * (p.gate ? gate_of(elem(static_cast<const T *>(p.gate)[at])) : 1.f));
         } else {
             p.part_o[part * p.D + d] = o;
         }
     }
     if (threadIdx.x == 0) {
         if (!whole) { p.part_ml[2 * part] = m; p.part_ml[2 * part + 1] = l; }
-        else if (LSE) LSE[(int64_t)b * p.Hq + h] = den > 0.f ? (m + log2f(den)) * kLn2 : -INFINITY;
+        else if (LSE) LSE[(int64_t)b * p.Hq + h] = end.lse;
     }
 }
 
@@ -249,16 +234,14 @@ k_paged_combine(const PagedParams p, T *__restrict__ O, float *__restrict__ LSE)
     const float base = m_keys == -INFINITY ? 0.f : m_keys;
     float l = 0.f;
     for (int i = 0; i < n; ++i) l += p.part_ml[2 * (part + i) + 1] * exp2f(p.part_ml[2 * (part + i)] - base);
-    float m = m_keys;
-    const float den = denominator<T>(m, l, p.sink, h);
-    const float inv = den > 0.f ? (m_keys == -INFINITY ? 0.f : exp2f(m_keys - m)) / den : 0.f;
+    const RowEnd end = row_end(m_keys, l, p.sink, h);
     for (int d = threadIdx.x; d < p.D; d += 128) {
         float o = 0.f;
         for (int i = 0; i < n; ++i) o = fmaf(p.part_o[(part + i) * p.D + d], exp2f(p.part_ml[2 * (part + i)] - base), o);
         const int64_t at = b * p.os_b + h * p.os_h + d;
-        from_f32(O[at], o * inv * (p.gate ? gate_of(elem(static_cast<const T *>(p.gate)[at])) : 1.f));
+        from_f32(O[at], o * end.factor * (p.gate ? gate_of(elem(static_cast<const T *>(p.gate)[at])) : 1.f));
     }
-    if (threadIdx.x == 0 && LSE) LSE[(int64_t)b * p.Hq + h] = den > 0.f ? (m + log2f(den)) * kLn2 : -INFINITY;
+    if (threadIdx.x == 0 && LSE) LSE[(int64_t)b * p.Hq + h] = end.lse;
 }
 
 cudaError_t combine(const PagedParams &p, hs2_dtype dt, void *O, float *LSE, cudaStream_t st)

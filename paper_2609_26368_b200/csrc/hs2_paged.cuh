@@ -61,6 +61,24 @@ __device__ __forceinline__ int2 paged_row(const PagedParams &p, int b, int j)
     return make_int2(page, j - col * p.ps);
 }
 
+// The end of a row whose keys are folded: l is the sum of their weights relative to `top` (log2 units, -inf without a key); the
+// sink joins the denominator as a key without a value.
+struct RowEnd {
+    float factor;   // of the sums of weighted values; 0 without a key
+    float lse;      // natural logarithm; -inf where there is nothing to sum
+};
+__device__ __forceinline__ RowEnd row_end(float top, float l, const float *sink, int h)
+{
+    float at = top, den = l;
+    if (sink) {
+        const float s2 = sink[h] * kLog2e;
+        at = fmaxf(top, s2);
+        if (at != -INFINITY || s2 != s2) den = l * exp2f(top - at) + exp2f(s2 - at);
+    }
+    // a denominator that is NaN (a logit or the sink was) is neither an empty one nor a factor of 0
+    return {l == 0.f ? 0.f : den > 0.f ? exp2f(top - at) / den : den, den == 0.f ? -INFINITY : (at + log2f(den)) * kLn2};
+}
+
 // e4m3: the power of two above the largest V scale, kept where it and its reciprocal are normal numbers
 __device__ __forceinline__ float v_unit_of(float top)
 {

@@ -576,14 +576,9 @@ k_paged_tc5(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
         float scale = 1.f;
         if (tid < n_heads) {
             if (whole) {
-                float den = sum, at = top;
-                if (p.sink) {   // the sink joins the denominator
-                    const float s2 = p.sink[h] * kLog2e;
-                    at = fmaxf(top, s2);
-                    if (at != -INFINITY) den = sum * exp2f(top - at) + exp2f(s2 - at);
-                }
-                scale = den > 0.f && top != -INFINITY ? exp2f(top - at) / den : (den != den ? den : 0.f);
-                if (LSE) LSE[(int64_t)b * p.Hq + h] = den > 0.f ? (at + log2f(den)) * kLn2 : -INFINITY;
+                const RowEnd end = row_end(top, sum, p.sink, h);
+                scale = end.factor;
+                if (LSE) LSE[(int64_t)b * p.Hq + h] = end.lse;
             } else {
                 const int64_t part = ((int64_t)b * p.Hq + h) * p.n_split + split;
                 p.part_ml[2 * part] = top;

@@ -163,14 +163,8 @@ k_window_simt(const Params p, int nf, int gp, int tq, const T *__restrict__ Q, c
         }
     }
     if (!mine) return;
-    float at_max = m, den = l;
-    if (sink) {   // the sink joins the denominator
-        const float s2 = sink[h] * kLog2e;
-        at_max = fmaxf(m, s2);
-        if (at_max != -INFINITY) den = l * exp2f(m - at_max) + exp2f(s2 - at_max);
-    }
-    const float inv = den > 0.f ? (m == -INFINITY ? 0.f : exp2f(m - at_max)) / den : 0.f;
-    if (LSE && part == 0) LSE[((int64_t)b * p.Hq + h) * p.Lq + i] = den > 0.f ? (at_max + log2f(den)) * kLn2 : -INFINITY;
+    const RowEnd the_end = row_end(m, l, sink, h);
+    if (LSE && part == 0) LSE[((int64_t)b * p.Hq + h) * p.Lq + i] = the_end.lse;
     const int64_t out = b * p.os_b + i * p.os_t + h * p.os_h;
 #pragma unroll
     for (int c = 0; c < DM / 16; ++c) {
@@ -178,7 +172,7 @@ k_window_simt(const Params p, int nf, int gp, int tq, const T *__restrict__ Q, c
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int d = 16 * c + 4 * part + e;
-            if (d < p.D) from_f32(O[out + d], x[e] * inv * (p.gate ? gate_of(to_f32(static_cast<const T *>(p.gate)[out + d])) : 1.f));
+            if (d < p.D) from_f32(O[out + d], x[e] * the_end.factor * (p.gate ? gate_of(to_f32(static_cast<const T *>(p.gate)[out + d])) : 1.f));
         }
     }
 }

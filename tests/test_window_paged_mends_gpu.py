@@ -178,3 +178,57 @@ def test_decode_of_a_query_that_is_not_a_number(case, n):
     assert out[0, 0, Hq - 1].isnan().all()
     out[0, 0, Hq - 1], lse[0, Hq - 1] = ref[0][0, 0, Hq - 1].to(dt).cuda(), ref[1][0, Hq - 1].cuda()
     plain_ops.check(out, lse, ref, D, "beside", p_eps=2.0 ** -8 if dt == BF16 else None)
+
+
+@pytest.mark.parametrize("n", [1, 40, 3000])
+@pytest.mark.parametrize("case", DECODES, ids=str)
+def test_decode_lse_of_what_is_not_a_number(case, n):
+    """NaN, not the -inf of a sequence without a key; the same for a NaN sink, where the output is NaN too."""
+    Hq, Hkv, D, dt, fp8, _ = case
+    g = torch.Generator().manual_seed(42)
+    lens = [n, 70, 0]
+    kx, vx, table, call = decode_setup(g, case, lens)
+    q = rand(g, 3, 1, Hq, D, dtype=dt)
+    sink = torch.randn(Hq, generator=g)
+    sink[1] = NAN
+    ref = plain_ops.paged(q, kx, vx, table, lens, 0, 0, D ** -0.5, sink)
+    out, lse = call(q, sink=sink.cuda())
+    assert out[:2, :, 1].isnan().all() and lse[:, 1].isnan().all()
+    keep = [h for h in range(Hq) if h != 1]
+    pick = (ref[0][:, :, keep], ref[1][:, keep], ref[2][:, :, keep], ref[3][:, keep])
+    plain_ops.check(out[:, :, keep], lse[:, keep], pick, D, "beside", p_eps=2.0 ** -8 if dt == BF16 else None)
+    q[0, 0, 0, 1] = NAN
+    out, lse = call(q)
+    assert lse[0, 0].isnan().all() and out[0, 0, 0].isnan().all() and not lse[1:, 0].isnan().any() and not lse[0, 2:].isnan().any()
+
+
+# a prompt's kernels: tcgen05 at three head dims, FMAs in bf16 and fp32; one token of the same layer
+WINDOWS = [(8, 2, 64, BF16, 90), (8, 1, 128, BF16, 90), (64, 1, 256, BF16, 90), (6, 2, 96, BF16, 90), (4, 2, 64, F32, 90), (8, 2, 128, BF16, 1),
+           (4, 2, 64, F32, 1)]
+
+
+@pytest.mark.parametrize("case", WINDOWS, ids=str)
+def test_window_of_queries_and_sinks_that_are_not_numbers(case):
+    Hq, Hkv, D, dt, Lq = case
+    g = torch.Generator().manual_seed(43)
+    Lk, w = 200, 50
+    q, k, v = rand(g, 1, Lq, Hq, D, dtype=dt), rand(g, 1, Lk, Hkv, D, dtype=dt), rand(g, 1, Lk, Hkv, D, dtype=dt)
+    sink = torch.randn(Hq, generator=g)
+    sink[1] = NAN
+    ref = plain_ops.window(q, k, v, w, 2, D ** -0.5, [Lk], [Lk - Lq], sink)
+    i = Lq // 2
+    q[0, i, 0, 5] = NAN
+    prob = hs2.Problem.from_tensors(q, k, 0, w)
+    out, lse = hs2.hs2_window_attn(prob, q.cuda(), k.cuda(), v.cuda(), 2, sink=sink.cuda(), want_lse=True)
+    assert out[:, :, 1].isnan().all() and out[0, i, 0].isnan().all()
+    assert lse[:, 1].isnan().all() and lse[0, 0, i].isnan()
+    fine = torch.ones(Lq, Hq, dtype=torch.bool)
+    fine[:, 1], fine[i, 0] = False, False
+    out[0, ~fine], lse[0, ~fine.T] = ref[0][0, ~fine].to(dt).cuda().nan_to_num(0.0), 0.0
+    ref = [x.clone() for x in ref]
+    ref[0][0, ~fine], ref[1][0, ~fine.T], ref[2][0, ~fine] = 0.0, 0.0, 0.0
+    out[0, ~fine] = 0.0
+    plain_ops.check(out, lse, ref, D, "beside")
+    # no sink: a NaN query's LSE is NaN there too
+    out, lse = hs2.hs2_window_attn(prob, q.cuda(), k.cuda(), v.cuda(), 2, want_lse=True)
+    assert out[0, i, 0].isnan().all() and lse[0, 0, i].isnan() and int(lse.isnan().sum()) == 1 and int(out.isnan().sum()) == D
