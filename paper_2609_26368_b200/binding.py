@@ -548,6 +548,7 @@ class PagedProblem:
         stride = page_table.stride()
         assert page_table.dtype == kv_lens.dtype == torch.int32 and page_table.is_cuda and rows == batch
         assert stride[1] == 1 or cols == 1
+        assert batch <= 1 or stride[0] >= cols, "the rows of the page table overlap: .contiguous() gives every sequence its own"
         assert kv_lens.is_contiguous() and tuple(kv_lens.shape) == (batch,) and kv_lens.device == page_table.device
         self.page_table, self.kv_lens = page_table, kv_lens
         self._cols, self._table_stride = cols, stride[0] if batch > 1 else max(stride[0], cols)

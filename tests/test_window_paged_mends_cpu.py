@@ -5,7 +5,10 @@ import shutil
 import subprocess
 
 import pytest
+import torch
+from torch._subclasses import FakeTensorMode
 
+import paper_2609_26368_b200 as hs2
 from paper_2609_26368_b200 import build as build_module
 
 INT_MAX = 2 ** 31 - 1
@@ -51,3 +54,22 @@ def test_released_entries_stay_in_the_row_for_any_keep(tmp_path):
         plain = range(-(-kept // ps), min(-(-held // ps), max_pages))   # without a limit on the numbers
         assert 0 <= end <= max_pages and 0 <= first <= max(end, -(-held // ps))
         assert max(0, end - first) == len(plain) and (not plain or first == plain[0])
+
+
+# ---------------------------------------------------------------- tensors that the library would read past
+@pytest.fixture
+def cuda():
+    """Tensors with shapes, strides and a CUDA device, and no memory."""
+    with FakeTensorMode(allow_non_fake_inputs=True):
+        yield lambda *shape, dtype=torch.bfloat16: torch.empty(*shape, dtype=dtype, device="cuda")
+
+
+def test_page_tables_with_shared_rows_are_refused(cuda):
+    """A row stride of 0 would say `packed` to the library, which would then take the rows from behind the one there is."""
+    row, lens = cuda(1, 8, dtype=torch.int32), cuda(4, dtype=torch.int32)
+    for table in (row.expand(4, 8), cuda(20, dtype=torch.int32).as_strided((4, 8), (4, 1)), cuda(4, 1, dtype=torch.int32)[:1].expand(4, 1)):
+        with pytest.raises(AssertionError):
+            hs2.PagedProblem(4, 8, 2, 64, 16, 100, table, lens)
+    for table in (cuda(4, 8, dtype=torch.int32), cuda(4, 20, dtype=torch.int32)[:, 5:13], cuda(4, 1, dtype=torch.int32)):
+        hs2.PagedProblem(4, 8, 2, 64, 16, 100, table, lens)
+    hs2.PagedProblem(1, 8, 2, 64, 16, 100, row.expand(1, 8), lens[:1])
