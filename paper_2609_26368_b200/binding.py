@@ -178,9 +178,20 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
+def _axes(strides, rows: int):
+    """``strides`` of a tensor of ``rows`` rows.  All of them 0 is `packed` to the library, which would read (or write) behind
+    the one row of a tensor that is broadcast along every axis."""
+    assert rows <= 1 or any(strides), "a tensor of one row, expanded: the library takes strides of 0 for packed"
+    return strides
+
+
 def _strides(t: torch.Tensor):
     assert t.stride(3) == 1, "last dimension must be contiguous"
-    return (C.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
+    return (C.c_int64 * 3)(*_axes(t.stride()[:3], t.shape[:3].numel()))
+
+
+def _scale_strides(t: torch.Tensor):
+    return (C.c_int64 * 3)(*_axes(t.stride(), t.numel()))
 
 
 class Problem:
@@ -334,7 +345,7 @@ def _sparse_fp8(fn_name, prob, q, k8, v8, k_scale, v_scale, idx, sink, out, lse,
     if lse is None and want_lse:
         lse = torch.empty(prob.batch, prob.n_q_heads, prob.q_len, dtype=torch.float32, device=q.device)
     c = prob.c_struct(q, k8, out)
-    c.kv_scale_stride = (C.c_int64 * 3)(*k_scale.stride())
+    c.kv_scale_stride = _scale_strides(k_scale)
     st = getattr(load_library(), fn_name)(C.byref(c), _dp(q), _dp(k8), _dp(v8), _dp(k_scale), _dp(v_scale), _dp(idx),
                                           _dp(sink), _dp(out), _dp(lse), _stream(stream))
     _check(st, fn_name)
@@ -361,7 +372,7 @@ def hs2_full_attn_select_fp8kv(prob: Problem, q, k8, v8, k_scale, v_scale, *, ou
     if idx is not None:
         ws = _workspace(prob, HS2_OP_FULL_ATTN_SELECT_FP8KV, dev, ws)
     c = prob.c_struct(q, k8, out)
-    c.kv_scale_stride = (C.c_int64 * 3)(*k_scale.stride())
+    c.kv_scale_stride = _scale_strides(k_scale)
     st = load_library().hs2_full_attn_select_fp8kv(C.byref(c), _dp(q), _dp(k8), _dp(v8), _dp(k_scale), _dp(v_scale), _dp(out),
                                                    _dp(lse), _dp(idx), _dp(ws), 0 if ws is None else ws.numel(), _stream(stream))
     _check(st, "hs2_full_attn_select_fp8kv")
@@ -498,6 +509,7 @@ def _outputs(q, out, sink, gate, lse, want_lse, n_q_heads, lse_shape):
         out = torch.empty_like(q if gate is None else gate)
     else:
         assert out.device == q.device
+        assert all(s or n == 1 for s, n in zip(out.stride(), out.shape)), "outputs of different rows share memory"
     if lse is None:
         if want_lse:
             lse = q.new_empty(lse_shape, dtype=torch.float32)
@@ -523,6 +535,8 @@ def hs2_window_attn(prob: Problem, q, k, v, n_first: int = 0, *, sink=None, gate
     out, lse = _outputs(q, out, sink, gate, lse, want_lse, Hq, (B, Hq, L))
     qs, ks, os_ = q.stride(), k.stride(), out.stride()
     assert qs[3] == ks[3] == 1, "last dimension must be contiguous"
+    _axes(qs[:3], B * L * Hq)
+    _axes(ks[:3], B * prob.kv_len * prob.n_kv_heads)
     c = _PROBLEM.pack(B, Hq, prob.n_kv_heads, prob.head_dim, L, prob.kv_len, prob.k_sel, prob.window, prob.softmax_scale,
                       _DTYPES[prob.dtype], _ptr(prob.q_start), _ptr(prob.kv_lens), *qs[:3], *ks[:3], *os_[:3], prob.select_block,
                       *_ZERO3)
@@ -560,8 +574,9 @@ class PagedProblem:
         return cls(B, Hq, Hkv, D, page_size, n_pages, page_table, kv_lens, dtype=q.dtype, **kw)
 
     def _pack(self, q=None, kv=None, o=None, scale=None) -> bytes:
-        q, o = ((0, 0) if t is None else t.stride()[0:4:2] for t in (q, o))
-        kv, scale = (_ZERO3 if t is None else t.stride()[:3] for t in (kv, scale))
+        q, o = ((0, 0) if t is None else _axes(t.stride()[0:4:2], self.batch * self.n_q_heads) for t in (q, o))
+        rows = self.n_pages * self.page_size * self.n_kv_heads
+        kv, scale = (_ZERO3 if t is None else _axes(t.stride()[:3], rows) for t in (kv, scale))
         return _PAGED.pack(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, self._cols,
                            self.window, self.n_first, self.softmax_scale, _DTYPES[self.dtype], self.page_table.data_ptr(),
                            self._table_stride, self.kv_lens.data_ptr(), *q, *o, *kv, *scale)

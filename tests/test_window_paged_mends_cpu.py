@@ -73,3 +73,33 @@ def test_page_tables_with_shared_rows_are_refused(cuda):
     for table in (cuda(4, 8, dtype=torch.int32), cuda(4, 20, dtype=torch.int32)[:, 5:13], cuda(4, 1, dtype=torch.int32)):
         hs2.PagedProblem(4, 8, 2, 64, 16, 100, table, lens)
     hs2.PagedProblem(1, 8, 2, 64, 16, 100, row.expand(1, 8), lens[:1])
+
+
+def test_tensors_broadcast_along_every_axis_are_refused(cuda):
+    """One row, or one scale, expanded to all: strides of 0, which the library takes for packed."""
+    B, Hq, Hkv, D, ps, n_pages, L = 3, 4, 2, 64, 16, 10, 20
+    table, lens = cuda(B, 4, dtype=torch.int32), cuda(B, dtype=torch.int32)
+    prob = hs2.PagedProblem(B, Hq, Hkv, D, ps, n_pages, table, lens)
+    one = cuda(1, 1, 1, D)
+    q, kv = cuda(B, 1, Hq, D), cuda(n_pages, ps, Hkv, D)
+    codes, scales = cuda(n_pages, ps, Hkv, D, dtype=torch.uint8), cuda(n_pages, ps, Hkv, dtype=torch.float32)
+    tensor_scale = cuda(1, dtype=torch.float32).expand(n_pages, ps, Hkv)
+    refused = "packed|share memory"
+    for args in ((one.expand(B, 1, Hq, D), kv, kv), (q, one.expand(n_pages, ps, Hkv, D), one.expand(n_pages, ps, Hkv, D))):
+        with pytest.raises(AssertionError, match=refused):
+            hs2.hs2_paged_attn_decode(prob, *args)
+    for out in (one.expand(B, 1, Hq, D), cuda(1, 1, Hq, D).expand(B, 1, Hq, D)):
+        with pytest.raises(AssertionError, match=refused):
+            hs2.hs2_paged_attn_decode(prob, q, kv, kv, out=out)
+    with pytest.raises(AssertionError, match=refused):
+        hs2.hs2_paged_attn_decode_fp8kv(prob, q, codes, codes, tensor_scale, tensor_scale)
+    wide = hs2.Problem(B, L, 50, Hq, Hkv, D, 0, 8)
+    wq, wkv = cuda(B, L, Hq, D), cuda(B, 50, Hkv, D)
+    for args, kw in (((one.expand(B, L, Hq, D), wkv, wkv), {}), ((wq, one.expand(B, 50, Hkv, D), one.expand(B, 50, Hkv, D)), {}),
+                     ((wq, wkv, wkv), dict(out=one.expand(B, L, Hq, D)))):
+        with pytest.raises(AssertionError, match=refused):
+            hs2.hs2_window_attn(wide, *args, **kw)
+    sparse = hs2.Problem(B, 1, 50, Hq, Hkv, 128, 0, 8)
+    codes, tensor_scale = cuda(B, 50, Hkv, 128, dtype=torch.uint8), cuda(1, dtype=torch.float32).expand(B, 50, Hkv)
+    with pytest.raises(AssertionError, match=refused):
+        hs2.hs2_sparse_attn_decode_fp8kv(sparse, cuda(B, 1, Hq, 128), codes, codes, tensor_scale, tensor_scale, None)
