@@ -367,7 +367,8 @@ hs2_status hs2_paged_attn_decode(const hs2_paged_problem *p, const void *Q, cons
 
 /* The same on an e4m3 cache (codes and one float scale per (token, KV head) for K and for V, packed or as records, as
  * for hs2_sparse_attn_decode_fp8kv); p->dtype describes Q, O and gate and must be HS2_BF16.  Tensor cores at head_dim
- * 128 and 256 with 16-byte aligned codes, fp32 FMAs elsewhere.  A scale below 2^-126 counts as zero. */
+ * 128 and 256 with 16-byte aligned codes, fp32 FMAs elsewhere.  A scale below 2^-126 counts as zero.  On tensor cores the weight
+ * of a key times its V scale, both relative to the largest, is an f16 operand: off by 2^-11 of itself down to 2^-23, by 2^-34 below. */
 hs2_status hs2_paged_attn_decode_fp8kv(const hs2_paged_problem *p, const void *Q, const void *K8, const void *V8,
                                        const float *k_scale, const float *v_scale, const float *sink, const void *gate,
                                        void *O, float *LSE, void *ws, size_t ws_bytes, void *cuda_stream);

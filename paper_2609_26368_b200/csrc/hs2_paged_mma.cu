@@ -11,8 +11,9 @@
 //     for), so a page may end anywhere in a tile.  Void rows (behind the chunk, bad pages) are zero-filled and masked.
 //   * online softmax in the base-2 domain; the key warps are joined through shared memory, the chunks by k_paged_combine.
 // e4m3: codes become f16 in registers (exact).  The K scale multiplies the score of its key; the V scale, relative to a
-// power of two above the largest one met so far, goes into the probability, which stays an f16 number of at most 1 then;
-// q is scaled into f16's range by a power of two per head.
+// power of two above the largest one met so far, goes into the probability, an f16 number of at most 1 then; all of them are 2^15
+// times that, so that they are normal f16 numbers (off by 2^-11) down to 2^-29 and are lost only below 2^-39.  q is scaled into
+// f16's range by a power of two per head.
 #include <cuda_fp16.h>
 
 #include "hs2_paged.cuh"
@@ -21,6 +22,7 @@ namespace hs2 {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 128;
+constexpr float kUpLog2 = 15.f, kDown = 0x1p-15f;   // of the probabilities on an e4m3 cache
 
 template <int D, bool F8, int NH, int WH>
 struct Cfg {
@@ -317,7 +319,7 @@ k_paged_mma(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
                     float pv[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        pv[e] = exp2f(s[mt][n][e] - use[e & 1]);
+                        pv[e] = exp2f(s[mt][n][e] - (F8 ? use[e & 1] - kUpLog2 : use[e & 1]));
                         l[n][e & 1] += pv[e];
                         if (F8) pv[e] *= vf[mt][e >> 1];
                     }
@@ -369,7 +371,7 @@ k_paged_mma(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
 
     float *so = reinterpret_cast<float *>(smem);
     float *sm = reinterpret_cast<float *>(smem + F::kBody + F::kRing), *sl = sm + kWarps * F::HEADS, *sf = sl + kWarps * F::HEADS;
-    const float unit = F8 ? v_unit : 1.f;
+    const float unit = F8 ? v_unit : 1.f, down = F8 ? kDown : 1.f;
 #pragma unroll
     for (int n = 0; n < NH; ++n)
 #pragma unroll
@@ -379,11 +381,11 @@ k_paged_mma(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
             sum += __shfl_xor_sync(0xffffffffu, sum, 4);
             sum += __shfl_xor_sync(0xffffffffu, sum, 8);
             sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-            if (g == 0) { sm[row] = m[n][hh]; sl[row] = sum; }
+            if (g == 0) { sm[row] = m[n][hh]; sl[row] = sum * down; }
 #pragma unroll
             for (int dt = 0; dt < KS; ++dt) {
-                so[row * F::kPitch + 16 * dt + (F8 ? 2 * g : g)] = o[n][dt][hh] * unit;
-                so[row * F::kPitch + 16 * dt + (F8 ? 2 * g + 1 : g + 8)] = o[n][dt][2 + hh] * unit;
+                so[row * F::kPitch + 16 * dt + (F8 ? 2 * g : g)] = o[n][dt][hh] * down * unit;
+                so[row * F::kPitch + 16 * dt + (F8 ? 2 * g + 1 : g + 8)] = o[n][dt][2 + hh] * down * unit;
             }
         }
     __syncthreads();

@@ -14,8 +14,10 @@
 //             the other copies are the same numbers and their P is zero here.  So 128 threads share the exponentials of 64
 //             heads, and each copy is a split of its own: own maximum, own denominator, own sums, joined at the end.
 //             Maximum kept lazily (O is rescaled only when it grows by more than 2^8).  e4m3: the K scale multiplies the
-//             score of its key, the V scale, relative to a power of two above the largest one met, the probability.
-// Measured (32 x 16K keys, head_dim 256, 64 heads): e4m3 97 us = 2.8 TB/s, bf16 112 us = 4.8 TB/s.  Bound by the chain of a
+//             score of its key, the V scale, relative to a power of two above the largest one met, the probability, an f16
+//             number: 2^10 times its value (and the maximum less lazy, 2^5), so that it is a normal one (off by 2^-11) down to 2^-24
+//             of the largest and is lost only below 2^-35.  2^7 and 2^8 would save 3 us of 100, 2^13 and 2^2 cost 26.
+// Measured (32 x 16K keys, head_dim 256, 64 heads): e4m3 99 us = 2.8 TB/s, bf16 115 us = 4.7 TB/s.  Bound by the chain of a
 // tile, which every tile of a CTA walks through: S 0.4 us, then 0.9 us of softmax, whose look-ups and exponentials wait on the
 // shared memory that the loaders' stores and the MMA's operands keep busy; the bf16 tiles are near the memory's rate.  A ring of
 // codes in shared memory instead of registers took 122 us where these took 104: a third more shared memory traffic.
@@ -33,7 +35,10 @@ namespace {
 using namespace tc5;
 
 constexpr int BM = 128, BN = 64;
-constexpr float kRescale = 8.f;   // log2 units
+// log2 units: how far a logit may be above the maximum in use; what the probabilities are multiplied by
+template <bool F8> constexpr float kRescale = F8 ? 5.f : 8.f;
+template <bool F8> constexpr float kUpLog2 = F8 ? 10.f : 0.f;
+template <bool F8> constexpr float kDown = F8 ? 0x1p-10f : 1.f;
 
 template <int D, bool F8>
 struct Cfg {
@@ -472,11 +477,12 @@ k_paged_tc5(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
                 top1 = max3(top1, s[e + 2], s[e + 3]);
             }
             const float top = fmaxf(top0, top1) * f_row;   // f_row is positive
-            const bool need = top > m_used + kRescale;   // also for the first visible key
+            const bool need = top > m_used + kRescale<F8>;   // also for the first visible key
             const bool grow = F8 && v_top > v_unit;
-            const float m_new = need ? top : m_used;
+            float m_new = m_used;
             if (__any_sync(0xffffffffu, need || grow)) {
-                const float corr_l = need ? exp2f(m_used - m_new) : 1.f;
+                m_new = fmaxf(m_used, top);   // of every row, while the warp is at it
+                const float corr_l = m_new > m_used ? exp2f(m_used - m_new) : 1.f;
                 l *= corr_l;
                 float corr = corr_l;
                 if (grow) {
@@ -500,7 +506,7 @@ k_paged_tc5(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
                 }
             }
             m_used = m_new;
-            const float base = m_used == -INFINITY ? 0.f : m_used, v_inv = F8 && v_unit > 0.f ? 1.f / v_unit : 0.f;
+            const float base = (m_used == -INFINITY ? 0.f : m_used) - kUpLog2<F8>, v_inv = F8 && v_unit > 0.f ? 1.f / v_unit : 0.f;
             uint32_t pk[NC / 2];
             float l0 = 0.f, l1 = 0.f;
 #pragma unroll
@@ -539,9 +545,9 @@ k_paged_tc5(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
     float *so = reinterpret_cast<float *>(smem);
     if (warp < 4) {
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-        const float scale = l == 0.f ? 0.f : F8 ? v_unit : 1.f;
+        const float scale = l == 0.f ? 0.f : F8 ? v_unit : 1.f, down = kDown<F8>;
         s_m[tid] = m_used;
-        s_l[tid] = l;
+        s_l[tid] = l * down;
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
             float o[32];
@@ -552,7 +558,7 @@ k_paged_tc5(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
                 *reinterpret_cast<float4 *>(so + tid * F::kPitch + c * 32 + e) = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) :
-                    make_float4(o[e] * scale, o[e + 1] * scale, o[e + 2] * scale, o[e + 3] * scale);
+                    make_float4(o[e] * down * scale, o[e + 1] * down * scale, o[e + 2] * down * scale, o[e + 3] * down * scale);
         }
     }
     tc_fence_before();

@@ -232,3 +232,27 @@ def test_window_of_queries_and_sinks_that_are_not_numbers(case):
     # no sink: a NaN query's LSE is NaN there too
     out, lse = hs2.hs2_window_attn(prob, q.cuda(), k.cuda(), v.cuda(), 2, want_lse=True)
     assert out[0, i, 0].isnan().all() and lse[0, 0, i].isnan() and int(lse.isnan().sum()) == 1 and int(out.isnan().sum()) == D
+
+
+# ---------------------------------------------------------------- e4m3 cache: what lies far below the largest probability
+@pytest.mark.parametrize("G, D", [(4, 128), (16, 128), (64, 128), (8, 256), (20, 256), (64, 256), (4, 64)])
+@pytest.mark.parametrize("below", [8.0, 15.7])
+def test_decode_fp8_long_tail_below_one_large_weight(G, D, below):
+    """One key holds nearly all of the weight and next to no value (a first token that heads park their attention on); the other
+    keys, e^-below of it each, carry the output.  Their weights are far from 2^-24 of the largest: none may be lost, and all are
+    rounded by 2^-11 of themselves."""
+    g = torch.Generator().manual_seed(44)
+    B, n, ps = 300, 1500, 100          # as many sequences as keep all keys of one in one CTA; they share their pages
+    q = torch.ones(B, 1, G, D, dtype=BF16)
+    c = below / D ** 0.5
+    k = -c + 0.1 * torch.randn(15, ps, 1, D, generator=g)
+    v = 1 + 0.2 * torch.randn(15, ps, 1, D, generator=g)
+    k[3, 7], v[3, 7] = 0.0, 1e-7
+    (k8, ks, kx), (v8, vs, vx) = quantise(k), quantise(v)
+    table = torch.randperm(15, generator=g).int().expand(B, 15).contiguous()
+    ref = plain_ops.paged(q[:1], kx, vx, table[:1], [n], 0, 0, D ** -0.5)
+    prob = hs2.PagedProblem.from_tensors(q, k8, table.cuda(), i32([n] * B))
+    out, lse = hs2.hs2_paged_attn_decode_fp8kv(prob, q.cuda(), k8.view(torch.uint8).cuda(), v8.view(torch.uint8).cuda(), ks.cuda(), vs.cuda(),
+                                               want_lse=True)
+    assert torch.equal(out, out[:1].expand_as(out))
+    plain_ops.check(out[:1], lse[:1], ref, D, "tail", p_eps=2.0 ** -11)
