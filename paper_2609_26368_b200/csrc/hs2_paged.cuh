@@ -85,6 +85,14 @@ __device__ __forceinline__ float v_unit_of(float top)
     return fmaxf(__uint_as_float(__float_as_uint(fminf(top, 0x1p124f)) & 0x7f800000u) * 2.f, 0x1p-126f);
 }
 
+// e4m3: what a row of q, largest magnitude `top` (NaN and infinities pass), is divided by to become an f16 operand of magnitudes
+// below 2^15, of which those down to 2^-29 of the largest are normal numbers: exact, as bf16 has fewer bits than f16.
+__device__ __forceinline__ float q_unit_of(float top)
+{
+    const float unit = __uint_as_float(__float_as_uint(top) & 0x7f800000u);   // the power of two at or below it
+    return fminf(fmaxf(unit, 0x1p-100f), 0x1p126f) * 0x1p-14f;
+}
+
 constexpr int kPagedMaxChunk = 2048;   // visible keys of one CTA at most: ragged batches then balance over many CTAs
 
 // Which groups run on the tcgen05 kernel.  Measured there and on mma.sync, us: head_dim 128, 64 x 16K keys: 32 heads 131 and 120

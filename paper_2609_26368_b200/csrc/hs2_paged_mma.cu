@@ -12,8 +12,8 @@
 //   * online softmax in the base-2 domain; the key warps are joined through shared memory, the chunks by k_paged_combine.
 // e4m3: codes become f16 in registers (exact).  The K scale multiplies the score of its key; the V scale, relative to a
 // power of two above the largest one met so far, goes into the probability, an f16 number of at most 1 then; all of them are 2^15
-// times that, so that they are normal f16 numbers (off by 2^-11) down to 2^-29 and are lost only below 2^-39.  q is scaled into
-// f16's range by a power of two per head.
+// times that, so that they are normal f16 numbers (off by 2^-11) down to 2^-29 and are lost only below 2^-39.  q becomes f16
+// in units of a power of two per head (q_unit_of).
 #include <cuda_fp16.h>
 
 #include "hs2_paged.cuh"
@@ -188,9 +188,7 @@ k_paged_mma(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
                 for (int e = 0; e < 2; ++e) top = fmaxf(top, fmaxf(fabsf(lo_bf16(qf[n][ks][e])), fabsf(hi_bf16(qf[n][ks][e]))));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            float unit = __uint_as_float(__float_as_uint(top) & 0x7f800000u);   // the power of two at or below it
-            if (!(unit > 0x1p-120f && unit < 0x1p120f)) unit = 1.f;
-            const float inv = 1.f / unit;
+            const float unit = q_unit_of(top), inv = 1.f / unit;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll

@@ -397,8 +397,7 @@ k_paged_tc5(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
                             top = __vmaxu2(top, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
                         }
                         const uint32_t most = max(top >> 16, top & 0xffffu) << 16;
-                        unit = __uint_as_float(most & 0x7f800000u);   // the power of two at or below it
-                        if (!(unit > 0x1p-110f && unit < 0x1p110f)) unit = 1.f;
+                        unit = q_unit_of(__uint_as_float(most));
                         inv = 1.f / unit;
                     }
                     f_row = unit * p.scale_log2;

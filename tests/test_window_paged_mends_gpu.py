@@ -135,7 +135,7 @@ DECODES = [(8, 2, 128, F32, False, 0), (3, 1, 80, BF16, False, 0), (8, 2, 128, B
            (64, 1, 128, BF16, False, 0), (40, 1, 256, BF16, True, 0), (4, 1, 256, BF16, False, 0)]                            # tcgen05
 
 
-def decode_setup(g, case, lens, ps=16):
+def decode_setup(g, case, lens, ps=16, **problem):
     """A cache of the case's kind, its values, and a call of the decode with a query."""
     Hq, Hkv, D, dt, fp8, shift = case
     n_pages = sum(-(-n // ps) for n in lens)
@@ -156,7 +156,7 @@ def decode_setup(g, case, lens, ps=16):
         room = torch.zeros(q.numel() + 8, dtype=dt, device="cuda")
         qd = room[shift:shift + q.numel()].view(q.shape)
         qd.copy_(q)
-        prob = hs2.PagedProblem.from_tensors(qd, args[0], table.cuda(), i32(lens))
+        prob = hs2.PagedProblem.from_tensors(qd, args[0], table.cuda(), i32(lens), **problem)
         return (hs2.hs2_paged_attn_decode_fp8kv if fp8 else hs2.hs2_paged_attn_decode)(prob, qd, *args, want_lse=True, **kw)
 
     return kx, vx, table, call
@@ -256,3 +256,22 @@ def test_decode_fp8_long_tail_below_one_large_weight(G, D, below):
                                                want_lse=True)
     assert torch.equal(out, out[:1].expand_as(out))
     plain_ops.check(out[:1], lse[:1], ref, D, "tail", p_eps=2.0 ** -11)
+
+
+@pytest.mark.parametrize("G, D", [(4, 128), (16, 128), (64, 128), (8, 256), (20, 256), (64, 256), (4, 64)])
+def test_decode_fp8_query_with_one_dimension_far_above_the_others(G, D):
+    """One dimension of q is 2^20 times the others, and the keys have next to nothing there: the logits come from the others."""
+    g = torch.Generator().manual_seed(47)
+    lens, ps = [700, 33], 16
+    kx = 300 * torch.randn(60, ps, 1, D, generator=g)
+    kx[..., 0] = 0.0
+    v = torch.randn(60, ps, 1, D, generator=g)
+    (k8, ks, kx), (v8, vs, vx) = quantise(kx), quantise(v)
+    q = rand(g, 2, 1, G, D, scale=0.001)
+    q[..., 0] = 1000.0
+    table = torch.randperm(60, generator=g).int()[:44].expand(2, 44).contiguous()
+    ref = plain_ops.paged(q, kx, vx, table, lens, 0, 0, 1.0)
+    prob = hs2.PagedProblem.from_tensors(q, k8, table.cuda(), i32(lens), softmax_scale=1.0)
+    out, lse = hs2.hs2_paged_attn_decode_fp8kv(prob, q.cuda(), k8.view(torch.uint8).cuda(), v8.view(torch.uint8).cuda(), ks.cuda(), vs.cuda(),
+                                               want_lse=True)
+    plain_ops.check(out, lse, ref, D, "query", p_eps=2.0 ** -11)
