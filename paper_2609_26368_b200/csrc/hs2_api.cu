@@ -86,7 +86,9 @@ hs2_status resolve_window(const hs2_problem *hp, Params *out)
     hs2_problem q = *hp;
     q.k_sel = 0;
     q.select_block = 0;
-    return resolve(&q, true, out);
+    const hs2_status s = resolve(&q, true, out);
+    if (s == HS2_OK) out->scale_log2 = fmaxf(out->scale_log2, 0x1p-126f);   // normal: -inf times a scale flushed to 0 would be NaN
+    return s;
 }
 
 int64_t select_rows(const Params &p) { return (int64_t)p.B * p.Hkv * p.Lq; }

@@ -27,7 +27,7 @@ hs2_status resolve(const hs2_paged_problem *hp, PagedParams *out)
     p.w = hp->window > 0 ? hp->window : INT_MAX;
     p.nf = hp->n_first;
     p.scale = hp->softmax_scale > 0.f ? hp->softmax_scale : 1.0f / sqrtf((float)p.D);
-    p.scale_log2 = p.scale * kLog2e;
+    p.scale_log2 = fmaxf(p.scale * kLog2e, 0x1p-126f);   // normal: -inf times a scale that is flushed to 0 would be NaN
     p.table = hp->page_table;
     p.table_stride = hp->table_stride > 0 ? hp->table_stride : hp->max_pages;
     p.kv_lens = hp->kv_lens;

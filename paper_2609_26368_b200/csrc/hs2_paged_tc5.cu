@@ -400,7 +400,7 @@ k_paged_tc5(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
                         unit = q_unit_of(__uint_as_float(most));
                         inv = 1.f / unit;
                     }
-                    f_row = unit * p.scale_log2;
+                    f_row = fmaxf(unit * p.scale_log2, 0x1p-126f);   // positive: void keys have logits of -inf
 #pragma unroll 1
                     for (int c = 0; c < PR; c += 4) {   // 16 columns
                         uint32_t w[16];

@@ -275,3 +275,32 @@ def test_decode_fp8_query_with_one_dimension_far_above_the_others(G, D):
     out, lse = hs2.hs2_paged_attn_decode_fp8kv(prob, q.cuda(), k8.view(torch.uint8).cuda(), v8.view(torch.uint8).cuda(), ks.cuda(), vs.cuda(),
                                                want_lse=True)
     plain_ops.check(out, lse, ref, D, "query", p_eps=2.0 ** -11)
+
+
+# ---------------------------------------------------------------- softmax scales
+@pytest.mark.parametrize("scale", [1e-30, 2e-38, 1e-40, 1e-45])
+@pytest.mark.parametrize("case", DECODES, ids=str)
+def test_decode_of_softmax_scales_next_to_zero(case, scale):
+    """All weights are equal then, and nothing is NaN: tiles with void rows and empty sequences included."""
+    Hq, Hkv, D, dt, fp8, _ = case
+    g = torch.Generator().manual_seed(48)
+    lens = [1, 70, 0]
+    kx, vx, table, call = decode_setup(g, case, lens, softmax_scale=scale)
+    q = rand(g, 3, 1, Hq, D, dtype=dt, scale=0.01)
+    ref = plain_ops.paged(q, kx, vx, table, lens, 0, 0, scale)
+    out, lse = call(q)
+    plain_ops.check(out, lse, ref, D, "equal weights", p_eps=2.0 ** -8 if dt == BF16 else None)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 2e-38, 1e-40, 1e-45])
+@pytest.mark.parametrize("case", WINDOWS, ids=str)
+def test_window_of_softmax_scales_next_to_zero(case, scale):
+    Hq, Hkv, D, dt, Lq = case
+    g = torch.Generator().manual_seed(49)
+    Lk, w = 200, 50
+    q, k, v = rand(g, 1, Lq, Hq, D, dtype=dt), rand(g, 1, Lk, Hkv, D, dtype=dt), rand(g, 1, Lk, Hkv, D, dtype=dt)
+    start = Lk - Lq - 20 if Lq > 1 else Lk - 1
+    ref = plain_ops.window(q, k, v, w, 2, scale, [Lk], [start])
+    prob = hs2.Problem.from_tensors(q, k, 0, w, softmax_scale=scale, q_start=i32([start]))
+    out, lse = hs2.hs2_window_attn(prob, q.cuda(), k.cuda(), v.cuda(), 2, want_lse=True)
+    plain_ops.check(out, lse, ref, D, "equal weights")
