@@ -315,7 +315,9 @@ hs2_status hs2_probe_gather(const hs2_problem *p, const void *K, const void *V, 
  *   sink    NULL or float [n_q_heads], gate NULL or logits laid out like O: both as for the sparse calls.
  *   O out; LSE out, NULL to skip (with the sink in it, as there).  A query that sees no key gets O = 0 and
  *           LSE = its sink (-inf without one).
- *   ws      only q_len == 1 uses scratch (HS2_OP_WINDOW_ATTN): the keys of a sequence are split over CTAs.
+ *   ws      only q_len == 1 uses scratch: the keys of a sequence are split over CTAs.  hs2_workspace_bytes(p, HS2_OP_WINDOW_ATTN)
+ *           is enough for any n_first; for one that is known, what it says of the same problem with kv_len =
+ *           min(kv_len, window + n_first).
  * bf16 at head_dim 64, 128 and 256 with 16-byte aligned tensors runs on tcgen05 (q_len > 1); every other shape up to
  * head_dim 256 and float32 run on fp32 FMAs.
  */

@@ -540,8 +540,11 @@ def hs2_window_attn(prob: Problem, q, k, v, n_first: int = 0, *, sink=None, gate
     c = _PROBLEM.pack(B, Hq, prob.n_kv_heads, prob.head_dim, L, prob.kv_len, prob.k_sel, prob.window, prob.softmax_scale,
                       _DTYPES[prob.dtype], _ptr(prob.q_start), _ptr(prob.kv_lens), *qs[:3], *ks[:3], *os_[:3], prob.select_block,
                       *_ZERO3)
-    if L == 1:
-        ws = _workspace(prob, HS2_OP_WINDOW_ATTN, q.device, ws)
+    if L == 1 and ws is None:   # scratch for the keys that can be visible
+        few = _CProblem.from_buffer_copy(c)
+        few.kv_len = min(prob.kv_len, prob.window + max(0, n_first))
+        n = load_library().hs2_workspace_bytes(C.byref(few), HS2_OP_WINDOW_ATTN)
+        ws = q.new_empty(n, dtype=torch.uint8) if n else None
     _launch("hs2_window_attn", q.device, stream, c, n_first, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(sink), _ptr(gate),
             out.data_ptr(), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel())
     return out, lse

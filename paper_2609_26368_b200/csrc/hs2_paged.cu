@@ -56,8 +56,10 @@ size_t paged_ws_bytes(const PagedParams &p) { return p.n_split <= 1 ? 0 : split_
 
 size_t paged_ws_bound(const PagedParams &p)
 {
-    const int64_t a = 3 * 4 * 148 / ((int64_t)p.B * p.Hkv) + 1, b = ((int64_t)p.max_len + kPagedMaxChunk - 1) / kPagedMaxChunk;
-    const int64_t n = a > b ? a : b;
+    // paged_plan's splits: at most three rounds of CTAs, at least a tile of keys each, or as many as the longest chunk asks for
+    const int64_t a = 3 * wave(p, false) / units(p, false), tiles = ((int64_t)p.max_len + kTile - 1) / kTile;
+    const int64_t b = ((int64_t)p.max_len + kPagedMaxChunk - 1) / kPagedMaxChunk;
+    const int64_t few = a < tiles ? a : tiles, n = few > b ? few : b;
     return n <= 1 ? 0 : split_bytes(p, n);
 }
 

@@ -102,7 +102,7 @@ inline bool paged_on_tc5(const PagedParams &p, bool fp8) { return (p.D == 256 &&
 // Fills chunk and n_split: the split that ends first if all contexts are as long as the table allows.
 void paged_plan(PagedParams *p, bool fp8);
 size_t paged_ws_bytes(const PagedParams &p);   // of a planned problem
-size_t paged_ws_bound(const PagedParams &p);   // of every plan with at most p.max_len visible keys
+size_t paged_ws_bound(const PagedParams &p);   // of every plan with at most p.max_len visible keys, cache not e4m3
 
 // K, V: elements of dtype `dt`, or e4m3 codes when ksc / vsc are given (dt then describes Q and O)
 cudaError_t launch_paged_decode(PagedParams p, hs2_dtype dt, const void *Q, const void *K, const void *V, const float *ksc,

@@ -1,4 +1,5 @@
 """CPU checks of host code and index arithmetic that the sliding-window, paged-decode and page calls share with their kernels."""
+import ctypes as C
 import os
 import random
 import shutil
@@ -9,6 +10,7 @@ import torch
 from torch._subclasses import FakeTensorMode
 
 import paper_2609_26368_b200 as hs2
+from paper_2609_26368_b200 import binding
 from paper_2609_26368_b200 import build as build_module
 
 INT_MAX = 2 ** 31 - 1
@@ -103,3 +105,44 @@ def test_tensors_broadcast_along_every_axis_are_refused(cuda):
     codes, tensor_scale = cuda(B, 50, Hkv, 128, dtype=torch.uint8), cuda(1, dtype=torch.float32).expand(B, 50, Hkv)
     with pytest.raises(AssertionError, match=refused):
         hs2.hs2_sparse_attn_decode_fp8kv(sparse, cuda(B, 1, Hq, 128), codes, codes, tensor_scale, tensor_scale, None)
+
+
+# ---------------------------------------------------------------- scratch
+@pytest.fixture(scope="module")
+def lib():
+    build_module.build()
+    return hs2.load_library()
+
+
+def window_ws(lib, **kw):
+    d = dict(batch=1, q_len=1, kv_len=131072, n_q_heads=64, n_kv_heads=1, head_dim=256, k_sel=0, window=128)
+    d.update(kw)
+    c = hs2.Problem(**d).c_struct()
+    return c, lib.hs2_workspace_bytes(C.byref(c), binding.HS2_OP_WINDOW_ATTN)
+
+
+def test_scratch_of_one_token_windows_follows_the_keys(lib):
+    """The bound was 1777 splits whatever the cache holds: 117 MB for a window of 128 tokens."""
+    assert window_ws(lib, kv_len=132)[1] <= 64 * 2 * 258 * 4
+    assert window_ws(lib, kv_len=128)[1] <= 64 * 258 * 4
+    assert window_ws(lib)[1] <= 64 * 444 * 258 * 4
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the pointers are not real")
+def test_scratch_of_one_token_windows_is_enough(lib):
+    """With the bytes that were named the call comes to look for a device; with what a plan has none of, it says so."""
+    rng, small = random.Random(2), 0
+    one = C.c_void_p(256)
+    for _ in range(3000):
+        n_kv, group = rng.choice([1, 2, 8]), rng.choice([1, 4, 8, 9, 16, 33, 64, 130])
+        kv_len, w, nf = rng.choice([1, 100, 129, 4000, 40000, 300000]), rng.choice([1, 128, 129, 4096, 100000]), rng.choice([0, 4, 500, 10 ** 6])
+        kw = dict(batch=rng.choice([1, 2, 5, 64, 400]), n_q_heads=n_kv * group, n_kv_heads=n_kv, head_dim=rng.choice([64, 80, 128, 256]),
+                  window=w, dtype=rng.choice([torch.float32, torch.bfloat16]))
+        c, most = window_ws(lib, kv_len=kv_len, **kw)
+        need = window_ws(lib, kv_len=min(kv_len, w + nf), **kw)[1]
+        assert need <= most
+        for n in (need, most):
+            st = lib.hs2_window_attn(C.byref(c), nf, one, one, one, None, None, one, None, one if n else None, n, None)
+            assert st == binding.HS2_ERR_CUDA, (kv_len, w, nf, kw)
+        small += lib.hs2_window_attn(C.byref(c), nf, one, one, one, None, None, one, None, None, 0, None) == binding.HS2_ERR_WORKSPACE_TOO_SMALL
+    assert small > 500
