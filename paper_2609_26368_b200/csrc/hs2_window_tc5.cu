@@ -207,49 +207,145 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap *tm, uint32_t src
                  ::"l"(tm), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 
-// Output columns 32 c + e of one query and head, for the bits e of `bad`, from its keys alone: the way out where the sum over
-// the tile is not finite.  Normalised, the sink included.  Mostly a value that the query does see is to blame: such a column is
-// settled by a look at the query's V rows (so that a call on NaNs throughout does not take minutes); the others, next to a
-// value that the query does not see, are computed in fp32.
+// Columns [32 c0, 32 c1) of one query and head again, from its keys alone, by a warp: the way out where the sum over the tile is not
+// finite, because of a value that the query may or may not see.  A column in which it does see one is settled by a look at the
+// query's V rows, at `hint` first, a key whose values were not finite in the row before (-1: none; the next hint is returned); where
+// a value that it does not see is to blame, its columns are computed in fp32, as on FMAs.  A lane has eight columns of every
+// kGroups-th key; the scores of 32 keys are a lane's each.  One NaN row of V under 64 heads on 1, head_dim 256, w = 4096, where the
+// layer takes 1.4 ms: 47 ms (1375 with a row per thread, a column after the other, while all other warps of the CTA wait).
 template <int D>
-__device__ __noinline__ void row_alone(const WindowArgs &a, const Item &t, int i, int h, int c, uint32_t bad, float (&o)[32])
+__device__ __noinline__ int row_alone(const WindowArgs &a, const Item &t, int i, int h, int row, char *buf, int c0, int hint)
 {
+    constexpr int kCols = D > 128 ? D / 2 : D, kPieces = kCols / 8, kGroups = 32 / kPieces;
     const Params &p = a.p;
-    const int pos = t.pos0 + (i - t.i0), end = min(pos + 1, t.kvl);
-    const int64_t head = t.b * p.ks_b + t.kvh * p.ks_h, behind = max((int64_t)0, (int64_t)pos - p.w + 1);
+    const int lane = threadIdx.x & 31, piece = lane % kPieces, group = lane / kPieces, col = c0 * 32 + piece * 8;
+    const int pos = t.pos0 + (i - t.i0), end = max(0, min(pos + 1, t.kvl));
+    const int lo = (int)max((int64_t)0, min((int64_t)pos - p.w + 1, (int64_t)end)), nf = min(a.nf, lo), n = nf + end - lo;
+    auto key = [&](int slot) { return (int64_t)(slot < nf ? slot : lo + (slot - nf)); };   // visible keys in order
     const __nv_bfloat16 *q = a.q + t.b * p.qs_b + i * p.qs_t + h * p.qs_h;
-    auto next = [&](int64_t j) { return j + 1 < a.nf || j + 1 >= behind ? j + 1 : behind; };   // visible keys in order
-    const int64_t first = a.nf > 0 ? 0 : behind;
-    uint32_t open = bad;                            // columns without a NaN so far
-    for (int e = 0; e < 32; ++e) o[e] = 0.f;
-    for (int64_t j = first; j < end && open; j = next(j))
-        for (uint32_t left = open; left; left &= left - 1) {
-            const int e = __ffs(left) - 1;
-            const float v = to_f32(a.v[head + j * p.ks_t + c * 32 + e]);
-            if (!(fabsf(v) < INFINITY)) o[e] += v;
-            if (o[e] != o[e]) open &= ~(1u << e);
+    const __nv_bfloat16 *kh = a.k + t.b * p.ks_b + t.kvh * p.ks_h, *vh = a.v + t.b * p.ks_b + t.kvh * p.ks_h + col;
+    auto words = [](const __nv_bfloat16 *x, uint32_t (&w)[4]) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(x));
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    };
+    float odd[8], o[8];                             // sums of the values that are not finite; of the others, weighted
+#pragma unroll
+    for (int e = 0; e < 8; ++e) odd[e] = o[e] = 0.f;
+    // adds what is not finite in 8 values; true once no column of the row can change any more
+    auto add = [&](const uint32_t (&v)[4]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = e & 1 ? hi_bf16(v[e >> 1]) : lo_bf16(v[e >> 1]);
+            if (!(fabsf(x) < INFINITY)) odd[e] += x;
         }
-    for (uint32_t left = open; left; left &= left - 1)
-        if (o[__ffs(left) - 1] != 0.f) open &= ~(left & -left);   // an infinity that it sees
-    if (!open) return;
-    float m = a.sink ? a.sink[h] * kLog2e : -INFINITY, l = m != -INFINITY ? 1.f : 0.f;
-    for (int pass = 0; pass < 2; ++pass)            // maximum and denominator, then the sums
-        for (int64_t j = first; j < end; j = next(j)) {
-            float s = 0.f;
-            for (int d = 0; d < D; ++d) s = fmaf(to_f32(q[d]), to_f32(a.k[head + j * p.ks_t + d]), s);
-            s *= p.scale_log2;
-            if (!pass) {
-                const float m_new = fmaxf(m, s);
-                if (m_new != -INFINITY) l = l * exp2f(m - m_new) + exp2f(s - m_new);
-                m = m_new;
-                continue;
+    };
+    auto settled = [&]() {
+        bool yes = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = odd[e];
+#pragma unroll
+            for (int d = kPieces; d < 32; d <<= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+            yes = yes && x != x;
+        }
+        return __all_sync(0xffffffffu, yes) != 0;
+    };
+    bool done = false;
+    if (hint >= 0 && hint < end && (hint >= lo || hint < nf)) {
+        uint32_t v[4];
+        words(vh + hint * p.ks_t, v);
+        if (group == 0) add(v);
+        done = settled();
+    }
+    constexpr int kAhead = 4;
+    for (int s0 = 0; s0 < n && !done; s0 += kGroups * kAhead) {
+        uint32_t v[kAhead][4];
+        int hit = -1;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int slot = s0 + u * kGroups + group;
+            v[u][0] = v[u][1] = v[u][2] = v[u][3] = 0u;
+            if (slot < n) words(vh + key(slot) * p.ks_t, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)             // an exponent of ones
+                if ((v[u][e] & 0x7f80u) == 0x7f80u || (v[u][e] & 0x7f800000u) == 0x7f800000u) hit = s0 + u * kGroups + group;
+        const uint32_t hits = __ballot_sync(0xffffffffu, hit >= 0);
+        if (!hits) continue;
+        hint = (int)key(__shfl_sync(0xffffffffu, hit, __ffs(hits) - 1));
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) add(v[u]);
+        done = settled();
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int d = kPieces; d < 32; d <<= 1) odd[e] += __shfl_xor_sync(0xffffffffu, odd[e], d);
+    bool open = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) open = open || odd[e] == 0.f;
+    if (__any_sync(0xffffffffu, open)) {
+        float m = -INFINITY, l = 0.f;
+        for (int s0 = 0; s0 < n; s0 += 32) {
+            float s = -INFINITY;
+            if (s0 + lane < n) {
+                const __nv_bfloat16 *k = kh + key(s0 + lane) * p.ks_t;
+                s = 0.f;
+#pragma unroll 4
+                for (int d = 0; d < D; d += 8) {
+                    uint32_t x[4], y[4];
+                    words(q + d, x);
+                    words(k + d, y);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s = fmaf(lo_bf16(x[e]), lo_bf16(y[e]), fmaf(hi_bf16(x[e]), hi_bf16(y[e]), s));
+                }
+                s *= p.scale_log2;
             }
-            const float w = m == -INFINITY ? 0.f : exp2f(s - m) / l;
-            for (uint32_t left = open; left; left &= left - 1) {
-                const int e = __ffs(left) - 1;
-                o[e] = fmaf(w, to_f32(a.v[head + j * p.ks_t + c * 32 + e]), o[e]);
+            const float m_new = fmaxf(m, warp_max(s)), base = m_new == -INFINITY ? 0.f : m_new, corr = exp2f(m - base), w = exp2f(s - base);
+            m = m_new;
+            l = l * corr + warp_sum(w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] *= corr;
+#pragma unroll 4
+            for (int u = 0; u < 32; u += kGroups) {
+                const float wu = __shfl_sync(0xffffffffu, w, u + group);
+                if (s0 + u + group < n) {
+                    uint32_t v[4];
+                    words(vh + key(s0 + u + group) * p.ks_t, v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        o[2 * e] = fmaf(wu, lo_bf16(v[e]), o[2 * e]);
+                        o[2 * e + 1] = fmaf(wu, hi_bf16(v[e]), o[2 * e + 1]);
+                    }
+                }
             }
         }
+        const float factor = row_end(m, l, a.sink, h).factor;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+#pragma unroll
+            for (int d = kPieces; d < 32; d <<= 1) o[e] += __shfl_xor_sync(0xffffffffu, o[e], d);
+            o[e] *= factor;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = odd[e] == 0.f ? o[e] : odd[e];   // (a NaN is not 0)
+    if (a.has_gate) {
+        uint32_t x[4];
+        words(static_cast<const __nv_bfloat16 *>(p.gate) + t.b * p.os_b + i * p.os_t + h * p.os_h + col, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[2 * e] *= gate_of(lo_bf16(x[e]));
+            o[2 * e + 1] *= gate_of(hi_bf16(x[e]));
+        }
+    }
+    const int at = col / 8;
+    if (group == 0)
+        *reinterpret_cast<uint4 *>(buf + (at >> 3) * (BM * 128) + row * 128 + (((at & 7) ^ (row & 7)) << 4)) =
+            make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
+    return hint;
 }
 
 // Columns [32 c0, 32 c1) of one row's output: O from tensor memory times 1 / denominator and the gate, as bf16 into the
@@ -258,29 +354,21 @@ template <int D>
 __device__ __forceinline__ void finish_row(const WindowArgs &a, const Item &t, uint32_t o_at, char *buf, int row, int i, int h, float inv, int c0,
                                            int c1)
 {
+    float odd = 0.f;                                            // NaN if any is not finite
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
         float o[32];
         tmem_ld32(o_at + c * 32, o);
         tmem_wait_ld();
-        float odd0 = 0.f, odd1 = 0.f, odd2 = 0.f, odd3 = 0.f;   // NaN if any is not finite
+        float odd0 = 0.f, odd1 = 0.f, odd2 = 0.f, odd3 = 0.f;
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
             odd0 = fmaf(o[e], 0.f, odd0); odd1 = fmaf(o[e + 1], 0.f, odd1);
             odd2 = fmaf(o[e + 2], 0.f, odd2); odd3 = fmaf(o[e + 3], 0.f, odd3);
         }
-        const float odd = (odd0 + odd1) + (odd2 + odd3);
+        odd += (odd0 + odd1) + (odd2 + odd3);
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] *= inv;
-        if (odd != 0.f && inv == inv && inv != 0.f && i < a.p.Lq && row < a.rows) {
-            uint32_t bad = 0;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) bad |= fabsf(o[e]) < INFINITY ? 0u : 1u << e;
-            float alone[32];   // (an array of its own: its address leaves, o stays in registers)
-            row_alone<D>(a, t, i, h, c, bad, alone);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = bad >> e & 1u ? alone[e] : o[e];   // normalised already
-        }
         if (inv == 0.f) {   // no key of its own: whatever 0 x V was
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = 0.f;
@@ -314,6 +402,14 @@ __device__ __forceinline__ void finish_row(const WindowArgs &a, const Item &t, u
             }
             *cell = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
         }
+    }
+    // (a row whose logits are NaN, or one without a key, has its answer)
+    const bool again = odd != 0.f && inv == inv && inv != 0.f && i < a.p.Lq && row < a.rows;
+    __syncwarp();
+    int hint = -1;
+    for (uint32_t rows = __ballot_sync(0xffffffffu, again); rows; rows &= rows - 1) {
+        const int src = __ffs(rows) - 1;
+        hint = row_alone<D>(a, t, __shfl_sync(0xffffffffu, i, src), __shfl_sync(0xffffffffu, h, src), row - (threadIdx.x & 31) + src, buf, c0, hint);
     }
 }
 
