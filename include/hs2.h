@@ -319,7 +319,7 @@ hs2_status hs2_probe_gather(const hs2_problem *p, const void *K, const void *V, 
  *           is enough for any n_first; for one that is known, what it says of the same problem with kv_len =
  *           min(kv_len, window + n_first).
  * bf16 at head_dim 64, 128 and 256 with 16-byte aligned tensors runs on tcgen05 (q_len > 1); every other shape up to
- * head_dim 256 and float32 run on fp32 FMAs.
+ * head_dim 256 and float32 run on fp32 FMAs.  q_len and kv_len are at most 2^31 - 2^22 (beyond: HS2_ERR_UNSUPPORTED).
  */
 hs2_status hs2_window_attn(const hs2_problem *p, int32_t n_first, const void *Q, const void *K, const void *V,
                            const float *sink, const void *gate, void *O, float *LSE, void *ws, size_t ws_bytes,
@@ -333,7 +333,8 @@ typedef struct {
     int32_t batch;
     int32_t n_q_heads, n_kv_heads, head_dim;   /* as in hs2_problem */
     int32_t page_size, n_pages;      /* tokens per page (any number >= 1), pages of the pool */
-    int32_t max_pages;               /* entries of a row of the page table that may be used; max_pages * page_size < 2^31 */
+    int32_t max_pages;               /* entries of a row of the page table that may be used; max_pages * page_size at most
+                                        2^31 - 2^22 (beyond: HS2_ERR_UNSUPPORTED), here and in hs2_page_pool */
     int32_t window;                  /* w: the new token and the w - 1 before it; 0 = the whole context */
     int32_t n_first;                 /* first tokens that stay visible behind the window */
     float softmax_scale;             /* 0 => 1/sqrt(head_dim) */
@@ -380,7 +381,8 @@ hs2_status hs2_paged_attn_decode_fp8kv(const hs2_paged_problem *p, const void *Q
  * packed.  A page is free when its count is 0.  The calls keep these invariants, given that they held before (zeroed
  * counts and lengths and a table of -1 are an empty pool): ref_counts[p] is the number of table entries that name p;
  * the first ceil(lens[s] / page_size) entries of row s are pages and the others are -1.  A table entry outside [0, n_pages)
- * is taken for -1.
+ * is taken for -1.  n_pages, max_seqs and the tokens of a call's rows are at most 2^31 - 2^22, the entries of a list 2^30 (beyond:
+ * HS2_ERR_UNSUPPORTED).
  */
 typedef struct {
     int32_t n_pages, page_size;

@@ -684,6 +684,7 @@ hs2_status hs2_window_attn(const hs2_problem *hp, int32_t n_first, const void *Q
     hs2_status s = resolve_window(hp, &p);
     if (s != HS2_OK) return s;
     if (n_first < 0 || !Q || !K || !V || !O) return HS2_ERR_INVALID_ARG;
+    if (p.Lk > kMaxIndex || p.Lq > kMaxIndex) return HS2_ERR_UNSUPPORTED;
     p.gate = gate;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;

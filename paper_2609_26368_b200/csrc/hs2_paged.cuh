@@ -8,6 +8,10 @@
 
 namespace hs2 {
 
+// Lengths, capacities and counts of pages and sequences end here: an index in tiles, or one grid further on, then stays in int32.
+constexpr int64_t kMaxIndex = (1ll << 31) - (1ll << 22);
+constexpr int32_t kMaxList = 1 << 30;   // entries of a list of sequences or pages
+
 // One new token per sequence against a cache in pages.  table == nullptr: page b is sequence b itself (a contiguous
 // cache of ps tokens per sequence).
 struct PagedParams {

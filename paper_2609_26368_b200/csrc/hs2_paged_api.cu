@@ -19,6 +19,7 @@ hs2_status resolve(const hs2_paged_problem *hp, PagedParams *out)
     if (!(hp->softmax_scale >= 0.f) || isinf(hp->softmax_scale)) return HS2_ERR_INVALID_ARG;
     if (hp->table_stride < 0 || (hp->table_stride > 0 && hp->table_stride < hp->max_pages)) return HS2_ERR_INVALID_ARG;
     if (!hp->page_table || !hp->kv_lens) return HS2_ERR_INVALID_ARG;
+    if ((int64_t)hp->max_pages * hp->page_size > kMaxIndex) return HS2_ERR_UNSUPPORTED;
     if (hp->head_dim > 256 || hp->batch > 65535 || hp->n_q_heads > 65535) return HS2_ERR_UNSUPPORTED;
     PagedParams p{};
     p.B = hp->batch; p.Hq = hp->n_q_heads; p.Hkv = hp->n_kv_heads; p.G = p.Hq / p.Hkv; p.D = hp->head_dim;
@@ -78,11 +79,13 @@ hs2_status run(PagedParams &p, hs2_dtype dt, const void *Q, const void *K, const
     return e == cudaSuccess ? HS2_OK : cuda_fail(e);
 }
 
-hs2_status check_pool(const hs2_page_pool *pool)
+hs2_status check_pool(const hs2_page_pool *pool, int32_t n = 0)
 {
     if (!pool || pool->n_pages <= 0 || pool->page_size <= 0 || pool->max_seqs <= 0 || pool->max_pages <= 0) return HS2_ERR_INVALID_ARG;
     if ((int64_t)pool->max_pages * pool->page_size > INT_MAX) return HS2_ERR_INVALID_ARG;
     if (!pool->ref_counts || !pool->page_table || !pool->lens) return HS2_ERR_INVALID_ARG;
+    if ((int64_t)pool->max_pages * pool->page_size > kMaxIndex || pool->n_pages > kMaxIndex || pool->max_seqs > kMaxIndex) return HS2_ERR_UNSUPPORTED;
+    if (n > kMaxList) return HS2_ERR_UNSUPPORTED;
     return HS2_OK;
 }
 
@@ -139,14 +142,14 @@ hs2_status hs2_paged_attn_decode_fp8kv(const hs2_paged_problem *hp, const void *
 
 size_t hs2_pages_workspace_bytes(const hs2_page_pool *pool, int32_t n)
 {
-    return check_pool(pool) != HS2_OK || n < 0 ? 0 : pages_ws_bytes(*pool, n);
+    return check_pool(pool, n) != HS2_OK || n < 0 ? 0 : pages_ws_bytes(*pool, n);
 }
 
 hs2_status hs2_pages_reserve(const hs2_page_pool *pool, const hs2_page_region *regions, int32_t n_regions,
                              const int32_t *seqs, const int32_t *n_new, int32_t n, int32_t *start, void *ws,
                              size_t ws_bytes, void *cuda_stream)
 {
-    hs2_status s = check_pool(pool);
+    hs2_status s = check_pool(pool, n);
     PageRegions rg;
     if (s != HS2_OK || (s = check_regions(*pool, regions, n_regions, &rg)) != HS2_OK) return s;
     if (n < 0 || (n > 0 && (!seqs || !n_new || !start))) return HS2_ERR_INVALID_ARG;
@@ -160,7 +163,7 @@ hs2_status hs2_pages_write(const hs2_page_pool *pool, const hs2_page_region *reg
                            const void *const *rows, const int64_t *row_strides, const int32_t *seqs, const int32_t *start,
                            const int32_t *n_new, int32_t n, int32_t max_new, void *cuda_stream)
 {
-    hs2_status s = check_pool(pool);
+    hs2_status s = check_pool(pool, n);
     PageRegions rg;
     if (s != HS2_OK || (s = check_regions(*pool, regions, n_regions, &rg)) != HS2_OK) return s;
     if (n < 0 || max_new < 0 || (n > 0 && (!seqs || !start || !n_new)) || (n_regions > 0 && (!rows || !row_strides))) return HS2_ERR_INVALID_ARG;
@@ -169,6 +172,7 @@ hs2_status hs2_pages_write(const hs2_page_pool *pool, const hs2_page_region *reg
         for (int k = 0; k < 3; ++k)
             if (row_strides[3 * r + k] % 4) return HS2_ERR_INVALID_ARG;
     }
+    if (max_new > kMaxIndex) return HS2_ERR_UNSUPPORTED;
     if ((s = check_device()) != HS2_OK) return s;
     const cudaError_t e = launch_pages_write(*pool, rg, rows, row_strides, seqs, start, n_new, n, max_new, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? HS2_OK : cuda_fail(e);
@@ -177,7 +181,7 @@ hs2_status hs2_pages_write(const hs2_page_pool *pool, const hs2_page_region *reg
 hs2_status hs2_pages_fork(const hs2_page_pool *pool, const int32_t *src, const int32_t *dst, int32_t n, void *ws,
                           size_t ws_bytes, void *cuda_stream)
 {
-    hs2_status s = check_pool(pool);
+    hs2_status s = check_pool(pool, n);
     if (s != HS2_OK) return s;
     if (n < 0 || (n > 0 && (!src || !dst))) return HS2_ERR_INVALID_ARG;
     if (!ws_ok(ws, ws_bytes, pages_ws_bytes(*pool, n))) return HS2_ERR_WORKSPACE_TOO_SMALL;
@@ -188,7 +192,7 @@ hs2_status hs2_pages_fork(const hs2_page_pool *pool, const int32_t *src, const i
 
 hs2_status hs2_pages_free(const hs2_page_pool *pool, const int32_t *seqs, const int32_t *keep, int32_t n, void *cuda_stream)
 {
-    hs2_status s = check_pool(pool);
+    hs2_status s = check_pool(pool, n);
     if (s != HS2_OK) return s;
     if (n < 0 || (n > 0 && !seqs)) return HS2_ERR_INVALID_ARG;
     if ((s = check_device()) != HS2_OK) return s;
@@ -211,7 +215,7 @@ hs2_status hs2_pages_compact(const hs2_page_pool *pool, const hs2_page_region *r
 hs2_status hs2_pages_copy(const hs2_page_pool *pool, const hs2_page_region *regions, int32_t n_regions, const int32_t *src,
                           const int32_t *dst, int32_t n, void *cuda_stream)
 {
-    hs2_status s = check_pool(pool);
+    hs2_status s = check_pool(pool, n);
     PageRegions rg;
     if (s != HS2_OK || (s = check_regions(*pool, regions, n_regions, &rg)) != HS2_OK) return s;
     if (n < 0 || (n > 0 && (!src || !dst))) return HS2_ERR_INVALID_ARG;

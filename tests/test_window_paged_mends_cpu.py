@@ -146,3 +146,45 @@ def test_scratch_of_one_token_windows_is_enough(lib):
             assert st == binding.HS2_ERR_CUDA, (kv_len, w, nf, kw)
         small += lib.hs2_window_attn(C.byref(c), nf, one, one, one, None, None, one, None, None, 0, None) == binding.HS2_ERR_WORKSPACE_TOO_SMALL
     assert small > 500
+
+
+# ---------------------------------------------------------------- sizes next to 2^31
+def test_sizes_whose_indices_would_wrap_are_refused(lib):
+    """Tiles and grids run past an end by up to 2^22: what lies closer to 2^31 than that is not supported."""
+    most, one, bad = 2 ** 31 - 2 ** 22, C.c_void_p(256), binding.HS2_ERR_UNSUPPORTED
+
+    def paged(**kw):
+        c = binding._CPagedProblem(2, 8, 2, 128, 1, 100, 10, 0, 0, 0.0, binding.HS2_BF16, 256, 0, 256)
+        for k, v in kw.items():
+            setattr(c, k, v)
+        return c
+
+    for c in (paged(max_pages=most + 1), paged(max_pages=INT_MAX), paged(page_size=most + 1, max_pages=1), paged(page_size=INT_MAX // 2, max_pages=2)):
+        assert lib.hs2_paged_attn_decode(C.byref(c), one, one, one, None, None, one, None, one, 1 << 62, None) == bad
+        assert lib.hs2_paged_workspace_bytes(C.byref(c)) == 0
+    assert lib.hs2_paged_workspace_bytes(C.byref(paged(max_pages=most))) > 0
+    w = hs2.Problem(1, 2, most + 1, 1, 1, 8, 0, 4).c_struct()
+    assert lib.hs2_window_attn(C.byref(w), 0, one, one, one, None, None, one, None, None, 0, None) == bad
+    w = hs2.Problem(1, most + 1, 2, 1, 1, 8, 0, 4).c_struct()
+    assert lib.hs2_window_attn(C.byref(w), 0, one, one, one, None, None, one, None, None, 0, None) == bad
+
+    def pool(**kw):
+        c = binding._CPagePool(100, 1, 8, 10, 256, 256, 256)
+        for k, v in kw.items():
+            setattr(c, k, v)
+        return c
+
+    g = binding._CPageRegion(256, 1, 256, 0, 1 << 50, 256)
+    for c, n in ((pool(n_pages=most + 1), 4), (pool(max_pages=most + 1), 4), (pool(max_seqs=INT_MAX), 4), (pool(), (1 << 30) + 1)):
+        assert lib.hs2_pages_workspace_bytes(C.byref(c), n) == 0
+        assert lib.hs2_pages_reserve(C.byref(c), C.byref(g), 1, one, one, n, one, one, 1 << 62, None) == bad
+        assert lib.hs2_pages_fork(C.byref(c), one, one, n, one, 1 << 62, None) == bad
+        assert lib.hs2_pages_free(C.byref(c), one, None, n, None) == bad
+        assert lib.hs2_pages_copy(C.byref(c), C.byref(g), 1, one, one, n, None) == bad
+        rows, strides = (C.c_void_p * 1)(256), (C.c_int64 * 3)(0, 1024, 256)
+        assert lib.hs2_pages_write(C.byref(c), C.byref(g), 1, rows, strides, one, one, one, n, 4, None) == bad
+        if n == 4:
+            assert lib.hs2_pages_compact(C.byref(c), C.byref(g), 1, None, one, 1 << 62, None) == bad
+    c = pool()
+    assert lib.hs2_pages_write(C.byref(c), C.byref(g), 1, rows, strides, one, one, one, 4, most + 1, None) == bad
+    assert lib.hs2_pages_workspace_bytes(C.byref(pool(n_pages=most, max_seqs=most)), 1 << 30) > 0
