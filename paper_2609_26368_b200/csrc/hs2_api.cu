@@ -218,7 +218,9 @@ void split_into_subgroups(Params *p, hs2_dtype dt)
     }
 }
 
-// The single-token form of the window layer is the paged decode on one page per sequence.
+// The single-token form of the window layer is the paged decode on one page per sequence; a grid has 65535 of them, and of heads,
+// at most, and more than that need no splits to fill a GPU: they run as a prompt of one token does.
+bool window_in_splits(const Params &p) { return p.B <= 65535 && p.Hq <= 65535; }
 PagedParams window_as_paged(const Params &p, int nf)
 {
     PagedParams d{};
@@ -278,7 +280,7 @@ size_t hs2_workspace_bytes(const hs2_problem *hp, hs2_op op)
         case HS2_OP_SPARSE_ATTN_PREFILL:
             return 0;
         case HS2_OP_WINDOW_ATTN:
-            if (resolve_window(hp, &p) != HS2_OK || p.Lq != 1) return 0;
+            if (resolve_window(hp, &p) != HS2_OK || p.Lq != 1 || !window_in_splits(p)) return 0;
             return paged_ws_bound(window_as_paged(p, p.Lk));   // any n_first
         case HS2_OP_FULL_ATTN_SELECT_FP8KV:
             if (resolve(hp, true, &p) != HS2_OK) return 0;
@@ -688,7 +690,7 @@ hs2_status hs2_window_attn(const hs2_problem *hp, int32_t n_first, const void *Q
     p.gate = gate;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
-    if (p.Lq == 1) {
+    if (p.Lq == 1 && window_in_splits(p)) {
         PagedParams d = window_as_paged(p, n_first);
         d.sink = sink;
         paged_plan(&d, false);
@@ -698,7 +700,7 @@ hs2_status hs2_window_attn(const hs2_problem *hp, int32_t n_first, const void *Q
     } else {
         if ((s = check_device()) != HS2_OK) return s;
         e = cudaErrorNotSupported;
-        if (window_tc5_supported(p, hp->dtype, Q, K, V, O)) e = launch_window_tc5(p, n_first, Q, K, V, sink, O, LSE, st);
+        if (p.Lq > 1 && window_tc5_supported(p, hp->dtype, Q, K, V, O)) e = launch_window_tc5(p, n_first, Q, K, V, sink, O, LSE, st);
         if (e == cudaErrorNotSupported) e = launch_window_simt(p, n_first, hp->dtype, Q, K, V, sink, O, LSE, st);
     }
     return e == cudaSuccess ? HS2_OK : cuda_fail(e);

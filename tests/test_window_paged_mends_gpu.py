@@ -337,3 +337,14 @@ def test_window_one_token_whose_values_are_not_finite(case, value, limit):
     # the others: once from tensor cores with weights in bf16, once in fp32 where they share a tile
     assert ((out.float() - clean).abs() <= 2.0 ** -7 * clean.abs() + (2.0 ** -8 + 2.0 ** -14) * A + 1e-30)[0, ~sees].all()
     assert t0.elapsed_time(t1) < limit
+
+
+# ---------------------------------------------------------------- more sequences or heads than a grid has rows
+@pytest.mark.parametrize("B, Hq, Hkv, D, Lk, dt", [(70000, 2, 1, 8, 5, F32), (65536, 1, 1, 64, 3, BF16), (1, 70000, 2, 8, 40, BF16)], ids=str)
+def test_window_of_one_token_for_very_many(B, Hq, Hkv, D, Lk, dt):
+    g = torch.Generator().manual_seed(51)
+    q, k, v = rand(g, B, 1, Hq, D, dtype=dt), rand(g, B, Lk, Hkv, D, dtype=dt), rand(g, B, Lk, Hkv, D, dtype=dt)
+    prob = hs2.Problem.from_tensors(q, k, 0, 3)
+    out, lse = hs2.hs2_window_attn(prob, q.cuda(), k.cuda(), v.cuda(), 1, want_lse=True)
+    o, l, A, S = plain_ops.window(q, k, v, 3, 1, D ** -0.5, [Lk] * B, [Lk - 1] * B)
+    plain_ops.check(out, lse, (o, l, A, S), D, "very many")
