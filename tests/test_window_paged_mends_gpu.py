@@ -135,17 +135,18 @@ DECODES = [(8, 2, 128, F32, False, 0), (3, 1, 80, BF16, False, 0), (8, 2, 128, B
            (64, 1, 128, BF16, False, 0), (40, 1, 256, BF16, True, 0), (4, 1, 256, BF16, False, 0)]                            # tcgen05
 
 
-def decode_setup(g, case, lens, ps=16, **problem):
+def decode_setup(g, case, lens, ps=16, table=None, **problem):
     """A cache of the case's kind, its values, and a call of the decode with a query."""
     Hq, Hkv, D, dt, fp8, shift = case
     n_pages = sum(-(-n // ps) for n in lens)
     k, v = rand(g, n_pages, ps, Hkv, D, dtype=F32 if fp8 else dt), rand(g, n_pages, ps, Hkv, D, dtype=F32 if fp8 else dt)
-    cols = max(1, max(-(-n // ps) for n in lens))
-    table, at = torch.full((len(lens), cols), -1, dtype=torch.int32), 0
-    for b, n in enumerate(lens):
-        m = -(-n // ps)
-        table[b, :m] = torch.arange(at, at + m, dtype=torch.int32)
-        at += m
+    if table is None:
+        cols, at = max(1, max(-(-n // ps) for n in lens)), 0
+        table = torch.full((len(lens), cols), -1, dtype=torch.int32)
+        for b, n in enumerate(lens):
+            m = -(-n // ps)
+            table[b, :m] = torch.arange(at, at + m, dtype=torch.int32)
+            at += m
     if fp8:
         (k8, ks, kx), (v8, vs, vx) = quantise(k), quantise(v)
         args = [k8.view(torch.uint8).cuda(), v8.view(torch.uint8).cuda(), ks.cuda(), vs.cuda()]
@@ -348,3 +349,45 @@ def test_window_of_one_token_for_very_many(B, Hq, Hkv, D, Lk, dt):
     out, lse = hs2.hs2_window_attn(prob, q.cuda(), k.cuda(), v.cuda(), 1, want_lse=True)
     o, l, A, S = plain_ops.window(q, k, v, 3, 1, D ** -0.5, [Lk] * B, [Lk - 1] * B)
     plain_ops.check(out, lse, (o, l, A, S), D, "very many")
+
+
+# ---------------------------------------------------------------- tables wider than the contexts
+@pytest.mark.parametrize("case", DECODES, ids=str)
+def test_decode_under_a_table_far_wider_than_the_contexts(case):
+    """A server's table has room for the longest sequence that it allows, which is what splits are planned for; what stands in it
+    behind the contexts is not read."""
+    Hq, Hkv, D, dt, fp8, _ = case
+    g = torch.Generator().manual_seed(52)
+    lens, ps = [4000, 1, 0, 700, 129], 16
+    kx, vx, table, _ = decode_setup(g, case, lens)
+    g = torch.Generator().manual_seed(52)
+    q = rand(g, len(lens), 1, Hq, D, dtype=dt)
+    ref = plain_ops.paged(q, kx, vx, table, lens, 0, 0, D ** -0.5)
+    for cols in (2048, 70000):
+        wide = torch.randint(-2 ** 31, 2 ** 31 - 1, (len(lens), cols), generator=g, dtype=torch.int64).int()
+        for b, n in enumerate(lens):
+            wide[b, :-(-n // ps)] = table[b, :-(-n // ps)]
+        out, lse = decode_setup(torch.Generator().manual_seed(52), case, lens, table=wide)[3](q)
+        plain_ops.check(out, lse, ref, D, "%d columns" % cols, p_eps=2.0 ** -8 if dt == BF16 else None)
+
+
+# ---------------------------------------------------------------- calls at the same time
+def test_windows_on_two_streams_at_once():
+    """Two layers whose CTAs run side by side, each taking row tiles from its own grid."""
+    g = torch.Generator().manual_seed(53)
+    jobs = []
+    for Hq, Hkv, D, w, gated in ((32, 4, 128, 40, True), (64, 1, 256, 60, True)):
+        q, k, v = rand(g, 1, 4000, Hq, D).cuda(), rand(g, 1, 4000, Hkv, D).cuda(), rand(g, 1, 4000, Hkv, D).cuda()
+        jobs.append((hs2.Problem.from_tensors(q, k, 0, w), q, k, v, rand(g, 1, 4000, Hq, D).cuda()))
+    want = [hs2.hs2_window_attn(p, q, k, v, 2, gate=gt, want_lse=True) for p, q, k, v, gt in jobs]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for n, (p, q, k, v, gt) in enumerate(jobs):
+            got[n].append(hs2.hs2_window_attn(p, q, k, v, 2, gate=gt, want_lse=True, stream=streams[n]))
+    torch.cuda.synchronize()
+    assert hs2.hs2_device_error_flags() == 0
+    for n in range(2):
+        for out, lse in got[n]:
+            assert torch.equal(out, want[n][0]) and torch.equal(lse, want[n][1])
