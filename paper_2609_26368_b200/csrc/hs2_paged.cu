@@ -217,7 +217,7 @@ k_paged_generic(const PagedParams p, const T *__restrict__ Q, const KV *__restri
     }
     if (threadIdx.x == 0) {
         if (!whole) { p.part_ml[2 * part] = m; p.part_ml[2 * part + 1] = l; }
-        else if (LSE) LSE[(int64_t)b * p.Hq + h] = end.lse;
+        else if (LSE) LSE[(int64_t)b * p.Hq + h] = end.lse();
     }
 }
 
@@ -243,7 +243,7 @@ k_paged_combine(const PagedParams p, T *__restrict__ O, float *__restrict__ LSE)
         const int64_t at = b * p.os_b + h * p.os_h + d;
         from_f32(O[at], o * end.factor * (p.gate ? gate_of(elem(static_cast<const T *>(p.gate)[at])) : 1.f));
     }
-    if (threadIdx.x == 0 && LSE) LSE[(int64_t)b * p.Hq + h] = end.lse;
+    if (threadIdx.x == 0 && LSE) LSE[(int64_t)b * p.Hq + h] = end.lse();
 }
 
 cudaError_t combine(const PagedParams &p, hs2_dtype dt, void *O, float *LSE, cudaStream_t st)

@@ -68,19 +68,22 @@ __device__ __forceinline__ int2 paged_row(const PagedParams &p, int b, int j)
 // The end of a row whose keys are folded: l is the sum of their weights relative to `top` (log2 units, -inf without a key); the
 // sink joins the denominator as a key without a value.
 struct RowEnd {
-    float factor;   // of the sums of weighted values; 0 without a key
-    float lse;      // natural logarithm; -inf where there is nothing to sum
+    float at, den;   // the maximum with the sink, and the denominator relative to it
+    float factor;    // of the sums of weighted values; 0 without a key
+    // natural logarithm of the whole; -inf where there is nothing to sum
+    __device__ __forceinline__ float lse() const { return den == 0.f ? -INFINITY : (at + log2f(den)) * kLn2; }
 };
 __device__ __forceinline__ RowEnd row_end(float top, float l, const float *sink, int h)
 {
-    float at = top, den = l;
+    RowEnd e{top, l, 0.f};
     if (sink) {
         const float s2 = sink[h] * kLog2e;
-        at = fmaxf(top, s2);
-        if (at != -INFINITY || s2 != s2) den = l * exp2f(top - at) + exp2f(s2 - at);
+        e.at = fmaxf(top, s2);
+        if (e.at != -INFINITY || s2 != s2) e.den = l * exp2f(top - e.at) + exp2f(s2 - e.at);
     }
     // a denominator that is NaN (a logit or the sink was) is neither an empty one nor a factor of 0
-    return {l == 0.f ? 0.f : den > 0.f ? exp2f(top - at) / den : den, den == 0.f ? -INFINITY : (at + log2f(den)) * kLn2};
+    if (l != 0.f) e.factor = e.den > 0.f ? exp2f(top - e.at) / e.den : e.den;
+    return e;
 }
 
 // e4m3: the power of two above the largest V scale, kept where it and its reciprocal are normal numbers

@@ -408,7 +408,7 @@ k_paged_mma(const PagedParams p, const __nv_bfloat16 *__restrict__ Q, const char
             if (whole) {
                 const RowEnd end = row_end(top, sum, p.sink, h);
                 scale = end.factor;
-                if (LSE) LSE[(int64_t)b * p.Hq + h] = end.lse;
+                if (LSE) LSE[(int64_t)b * p.Hq + h] = end.lse();
             } else {
                 const int64_t part = ((int64_t)b * p.Hq + h) * p.n_split + split;
                 p.part_ml[2 * part] = top;

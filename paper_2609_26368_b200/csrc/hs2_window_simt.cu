@@ -164,7 +164,7 @@ k_window_simt(const Params p, int nf, int gp, int tq, const T *__restrict__ Q, c
     }
     if (!mine) return;
     const RowEnd the_end = row_end(m, l, sink, h);
-    if (LSE && part == 0) LSE[((int64_t)b * p.Hq + h) * p.Lq + i] = the_end.lse;
+    if (LSE && part == 0) LSE[((int64_t)b * p.Hq + h) * p.Lq + i] = the_end.lse();
     const int64_t out = b * p.os_b + i * p.os_t + h * p.os_h;
 #pragma unroll
     for (int c = 0; c < DM / 16; ++c) {

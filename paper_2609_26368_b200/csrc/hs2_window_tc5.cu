@@ -739,7 +739,7 @@ k_window_tc5(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
                 r += 2 * t.n_blk;
                 const int i = t.i0 + q_in, h = t.h0 + h_in;
                 const RowEnd end = row_end(m_used, l, a.sink, h);   // (h_in is below gp in the rows behind the last one too)
-                if (a.lse && i < p.Lq && row < a.rows && ok) a.lse[((int64_t)t.b * p.Hq + h) * p.Lq + i] = end.lse;
+                if (a.lse && i < p.Lq && row < a.rows && ok) a.lse[((int64_t)t.b * p.Hq + h) * p.Lq + i] = end.lse();
                 const float inv = end.factor;
                 if constexpr (F::kEpi) {   // hand it over; the epilogue of the row tile before has read its own by then
                     if (ok && k > 0) ok = __all_sync(0xffffffffu, wait(bar(STAT_FREE), (k - 1) & 1, abort_flag));
