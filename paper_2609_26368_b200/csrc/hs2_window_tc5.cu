@@ -348,13 +348,49 @@ __device__ __noinline__ int row_alone(const WindowArgs &a, const Item &t, int i,
     return hint;
 }
 
+// What finish_row leaves to be done again, of a warp's rows: gates of which a logit is NaN or too low for the paired form (`low`), and
+// rows of which a sum is not finite (`alone`).  Out of the way of all others: in finish_row's loop the two cost every call 2 to 4 %.
+template <int D>
+__device__ __noinline__ void finish_again(const WindowArgs &a, const Item &t, uint32_t o_at, char *buf, int row, int i, int h, float inv, int c0, int c1,
+                                          bool alone, bool low)
+{
+    if (__any_sync(0xffffffffu, low)) {
+        const __nv_bfloat16 *gate = static_cast<const __nv_bfloat16 *>(a.p.gate) + t.b * a.p.os_b + i * a.p.os_t + h * a.p.os_h;
+#pragma unroll 1
+        for (int c = 2 * c0; c < 2 * c1; ++c) {   // 16 columns
+            float o[16];
+            tmem_ld16(o_at + c * 16, o);
+            tmem_wait_ld();
+            if (low) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = (inv == 0.f ? 0.f : o[e] * inv) * gate_of(to_f32(gate[c * 16 + e]));
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const float *f = o + 8 * q;
+                    const int at = 2 * c + q;
+                    *reinterpret_cast<uint4 *>(buf + (at >> 3) * (BM * 128) + row * 128 + (((at & 7) ^ (row & 7)) << 4)) =
+                        make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+                }
+            }
+            __syncwarp();
+        }
+    }
+    __syncwarp();
+    int hint = -1;
+    for (uint32_t rows = __ballot_sync(0xffffffffu, alone); rows; rows &= rows - 1) {
+        const int src = __ffs(rows) - 1;
+        hint = row_alone<D>(a, t, __shfl_sync(0xffffffffu, i, src), __shfl_sync(0xffffffffu, h, src), row - (threadIdx.x & 31) + src, buf, c0, hint);
+    }
+}
+
 // Columns [32 c0, 32 c1) of one row's output: O from tensor memory times 1 / denominator and the gate, as bf16 into the
 // row's place in the swizzled buffer `buf` (which holds the gate until then).
 template <int D>
 __device__ __forceinline__ void finish_row(const WindowArgs &a, const Item &t, uint32_t o_at, char *buf, int row, int i, int h, float inv, int c0,
                                            int c1)
 {
-    float odd = 0.f;                                            // NaN if any is not finite
+    float odd = 0.f;                         // NaN if any is not finite
+    uint32_t least = 0u;                     // the least gate logits (or 0), NaN if any is
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
         float o[32];
@@ -382,35 +418,23 @@ __device__ __forceinline__ void finish_row(const WindowArgs &a, const Item &t, u
             if (a.has_gate) {
                 const uint4 gt = *cell;
                 const uint32_t wd[4] = {gt.x, gt.y, gt.z, gt.w};
-                const uint32_t least = min_bf16x2(min_bf16x2(gt.x, gt.y), min_bf16x2(gt.z, gt.w));
-                if (lo_bf16(least) > kPairedGate && hi_bf16(least) > kPairedGate) {
-                    // 1 / (1 + e^-x) and 1 / (1 + e^-y) with one reciprocal: the exponential unit is the busiest one here
+                least = min_bf16x2(least, min_bf16x2(min_bf16x2(gt.x, gt.y), min_bf16x2(gt.z, gt.w)));
+                // 1 / (1 + e^-x) and 1 / (1 + e^-y) with one reciprocal: the exponential unit is the busiest one here
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float u = 1.f + exp2f(lo_bf16(wd[e]) * -kLog2e), v = 1.f + exp2f(hi_bf16(wd[e]) * -kLog2e);
-                        const float inv_uv = __fdividef(1.f, u * v);
-                        f[2 * e] *= v * inv_uv;
-                        f[2 * e + 1] *= u * inv_uv;
-                    }
-                } else {   // NaN too.  (One look at eight logits: 64 heads on 1, head_dim 256, 8K, w = 128 206 us; one at each pair 246)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        f[2 * e] *= gate_of(lo_bf16(wd[e]));
-                        f[2 * e + 1] *= gate_of(hi_bf16(wd[e]));
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const float u = 1.f + exp2f(lo_bf16(wd[e]) * -kLog2e), v = 1.f + exp2f(hi_bf16(wd[e]) * -kLog2e);
+                    const float inv_uv = __fdividef(1.f, u * v);
+                    f[2 * e] *= v * inv_uv;
+                    f[2 * e + 1] *= u * inv_uv;
                 }
             }
             *cell = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
         }
     }
-    // (a row whose logits are NaN, or one without a key, has its answer)
-    const bool again = odd != 0.f && inv == inv && inv != 0.f && i < a.p.Lq && row < a.rows;
-    __syncwarp();
-    int hint = -1;
-    for (uint32_t rows = __ballot_sync(0xffffffffu, again); rows; rows &= rows - 1) {
-        const int src = __ffs(rows) - 1;
-        hint = row_alone<D>(a, t, __shfl_sync(0xffffffffu, i, src), __shfl_sync(0xffffffffu, h, src), row - (threadIdx.x & 31) + src, buf, c0, hint);
-    }
+    // (a row whose logits are NaN, or one without a key, has its sums)
+    const bool mine = i < a.p.Lq && row < a.rows, alone = odd != 0.f && inv == inv && inv != 0.f && mine;
+    const bool low = mine && !(lo_bf16(least) > kPairedGate && hi_bf16(least) > kPairedGate);
+    if (__any_sync(0xffffffffu, alone || low)) finish_again<D>(a, t, o_at, buf, row, i, h, inv, c0, c1, alone, low);
 }
 
 template <int D>
