@@ -45,7 +45,7 @@ __device__ __forceinline__ PagedKeys paged_keys(const PagedParams &p, int b)
 {
     const int given = p.kv_lens ? p.kv_lens[b] : p.max_len;
     const int len = given < 0 ? 0 : (given > p.max_len ? p.max_len : given);
-    int pos = p.q_start ? p.q_start[b] : len - 1;
+    int pos = p.q_start ? p.q_start[b] : (p.table || given < 0 ? len : given) - 1;   // (the window layer's is not held to the cache)
     if (pos < -1) pos = -1;
     const int end = pos < len ? pos + 1 : len;   // keys 0 .. end - 1
     PagedKeys k;

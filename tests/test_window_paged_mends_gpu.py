@@ -391,3 +391,17 @@ def test_windows_on_two_streams_at_once():
     for n in range(2):
         for out, lse in got[n]:
             assert torch.equal(out, want[n][0]) and torch.equal(lse, want[n][1])
+
+
+# ---------------------------------------------------------------- lengths beyond the cache
+@pytest.mark.parametrize("Lq", [1, 3])
+@pytest.mark.parametrize("D, dt", [(128, BF16), (64, F32), (96, BF16)], ids=str)
+def test_window_of_lengths_beyond_the_cache(D, dt, Lq):
+    """Without q_start the last query stands at kv_lens[b] - 1, wherever the cache ends: for one token as for a prompt."""
+    g = torch.Generator().manual_seed(54)
+    B, Lk, w = 4, 60, 20
+    q, k, v = rand(g, B, Lq, 8, D, dtype=dt), rand(g, B, Lk, 2, D, dtype=dt), rand(g, B, Lk, 2, D, dtype=dt)
+    lens = [Lk, Lk + 7, Lk + 40, 2 ** 31 - 1]
+    ref = plain_ops.window(q, k, v, w, 1, D ** -0.5, [min(n, Lk) for n in lens], [n - Lq for n in lens])
+    out, lse = hs2.hs2_window_attn(hs2.Problem.from_tensors(q, k, 0, w, kv_lens=i32(lens)), q.cuda(), k.cuda(), v.cuda(), 1, want_lse=True)
+    plain_ops.check(out, lse, ref, D, "beyond")
