@@ -351,7 +351,9 @@ typedef struct {
 } hs2_paged_problem;
 
 /* Bytes of scratch the paged decode calls need: the un-normalised partial results of the splits of the longest
- * context the page table can hold.  A host-side computation; 0 is a valid answer, and the answer for an invalid problem. */
+ * context the page table can hold (in all sequences at once: 64 sequences of 64 heads at head_dim 256 take 270 MB under tables
+ * for 128K tokens each).  A host-side computation; 0 is a valid answer, and the answer for an invalid problem.  The splits are
+ * planned for that context too: under tables far wider than the contexts few sequences fill few SMs. */
 size_t hs2_paged_workspace_bytes(const hs2_paged_problem *p);
 
 /*
@@ -361,7 +363,8 @@ size_t hs2_paged_workspace_bytes(const hs2_paged_problem *p);
  *   Q, O    [batch, 1, n_q_heads, head_dim]; sink, gate, LSE (float [batch, n_q_heads, 1], nullable) as for the sparse calls.
  *   kv_lens[b] is clamped to [0, max_pages * page_size].  A page_table entry outside [0, n_pages) voids the tokens of its
  *   page: they are left out of the softmax, and nothing is read for them.  Entries behind kv_lens[b] are not read.
- *   A sequence without a visible token gets O = 0, LSE = its sink (-inf without one).
+ *   A sequence without a visible token gets O = 0, LSE = its sink (-inf without one).  A NaN in a logit or the sink makes O
+ *   and LSE of its head NaN; an infinite value that is visible makes its column of O infinite or NaN.
  * bf16 at head_dim 64, 128 and 256 with 16-byte aligned tensors runs on tensor cores; everything else up to head_dim
  * 256, and float32, on fp32 FMAs.
  */

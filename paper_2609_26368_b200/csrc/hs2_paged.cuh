@@ -103,8 +103,9 @@ __device__ __forceinline__ float q_unit_of(float top)
 constexpr int kPagedMaxChunk = 2048;   // visible keys of one CTA at most: ragged batches then balance over many CTAs
 
 // Which groups run on the tcgen05 kernel.  Measured there and on mma.sync, us: head_dim 128, 64 x 16K keys: 32 heads 131 and 120
-// (e4m3: 116, 108), 64 heads 138 and 185 (124, 186); head_dim 256, 32 x 16K: 8 heads 101 and 113 (86, 64), 16 heads 103 and 131
-// (87, 77), 32 heads 105 and 130 (88, 111).  One sequence of 4K keys, 8 heads at head_dim 256: 18.6 and 16.6.
+// (e4m3: 116, 108), 64 heads 137 and 185 (126, 186); head_dim 256, 32 x 16K: 8 heads 100 and 111 (86, 64), 16 heads 101 and 128
+// (87, 77), 32 heads 105 and 130 (90, 111).  By the shape alone, although one short sequence is faster on mma.sync: bf16, 8 heads at
+// head_dim 256, 1 x 100 keys 8.4 and 7.0, 1 x 4K 15.8 and 14.2; but 1 x 32K 35 and 59, 8 x 4K 16.2 and 20.7.
 inline bool paged_on_tc5(const PagedParams &p, bool fp8) { return (p.D == 256 && (p.G > 16 || !fp8)) || (p.D == 128 && p.G > 32); }
 // Fills chunk and n_split: the split that ends first if all contexts are as long as the table allows.
 void paged_plan(PagedParams *p, bool fp8);

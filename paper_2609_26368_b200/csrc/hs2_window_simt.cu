@@ -2,10 +2,10 @@
 //
 // A row tile of 32 rows is TQ consecutive queries x GP heads of one group (as on tcgen05), a key tile is 32 keys; both come to
 // shared memory as fp32, head_dim padded to a multiple of 16 with zeros.  Four threads share a row: each takes eight of a tile's
-// scores, the row's maximum and sum meet by shuffles, then each takes a quarter of the output's dimensions.  A value is used 8
-// (K, V) or 32 times (Q) per load from shared memory, which is what bounds the kernel: two 16-byte reads in nine FMAs of four.
-// Measured, fp32, head_dim 64: 12 heads on 2, 2400 tokens, w = 512: 283 us (1703 with a warp per query); 4 heads on 1, 512 tokens,
-// w = 16: 14.5 us (12.4), the latency of two key tiles.
+// scores, the row's maximum and sum meet by shuffles, then each takes a quarter of the output's dimensions.  What bounds the kernel
+// is shared memory: nine 16-byte reads to 32 FMAs in Q K^T, one to four in P V.
+// Measured, fp32, head_dim 64: 12 heads on 2, 2400 tokens, w = 512: 272 us (1703 with a warp per query); 4 heads on 1, 512 tokens,
+// w = 16: 14.5 us (12.4), the latency of two key tiles.  bf16, head_dim 96, 32 heads on 4, 8K tokens: w = 128 1.13 ms, w = 1024 6.7 ms.
 #include <limits.h>
 
 #include "hs2_paged.cuh"

@@ -10,7 +10,8 @@
 //   schedule   CTAs (one per SM at head_dim 256, two below) take row tiles one after the other: the grid has a CTA per
 //              row tile, and a running CTA cancels the launch of the next one and does its work
 //              (clusterlaunchcontrol.try_cancel), asked for one row tile ahead.
-//   TMA warp   Q into one of two buffers, a row tile ahead, a ring of K / V tiles, K ahead of V, and the gate, into the row
+//   TMA warp   Q into one of two buffers, the next row tile's while this one's last key tile is in work (at head_dim 256: as soon as
+//              the output of the row tile before has left), a ring of K / V tiles, K ahead of V, and the gate, into the row
 //              tile's Q buffer once its last Q K^T has run.
 //   MMA warp   S = Q K^T into one of 2 to 4 score buffers, ahead of O += P V (P in tensor memory, over the scores it came
 //              from), into the next row tile too: while the epilogue holds O, the next row tile's scores and P are made.
@@ -18,10 +19,12 @@
 //              when a row's maximum grew by more than 2^8), P back to tensor memory as bf16.
 //   epilogue   O / l times the gate, through shared memory and a TMA store: by the softmax warps where a second CTA covers
 //              them, by 8 warps of its own at head_dim 256.  The output leaves from the row tile's Q buffer, where the gate is.
-// Measured, us (and the bytes' or products' time at the device's rates): 64 heads on 1, head_dim 256, 8K tokens, w = 128: 158 (83),
-// with a gate 198 (125), w = 512: 303 (159); 32 on 4, head_dim 128: 8K, w = 128: 54 (21), w = 1024: 149 (77); 32K, w = 128: 205 (83).
+// Measured, us (and the bytes' or products' time at the device's rates): 64 heads on 1, head_dim 256, 8K tokens, w = 128: 156 (83),
+// with a gate 192 (125), w = 512: 300 (159); 32 on 4, head_dim 128: 8K, w = 128: 54 (21), w = 1024: 154 (77); 32K, w = 128: 203 (83).
 // A narrow window is bound by the chain of a row tile (scores, softmax, P V, epilogue: some 7 us for its 3 key tiles at head_dim
-// 256, of which a CTA keeps two in work), a wide one by the exponentials, which take as long as the products.
+// 256, of which a CTA keeps two in work).  At head_dim 128 a row tile costs its SM 2.4 us and 0.5 us per key tile: a key tile is what
+// it is in the full layer's kernel, the fixed part three fifths of w = 128 and a fifth of w = 1024.  P is bf16, V's type on the tensor
+// cores: off by 2^-9 of itself, which over many keys moves an output by less than its own rounding.
 // What lies behind a cache's end may be anything: keys are masked by selection, V rows are zeroed in shared memory.  A V
 // row that is not finite would reach neighbouring queries of the tile as 0 x inf: a row whose sum is not finite is looked
 // at again, over its own keys alone.  Behind the first tokens, which end inside a tile, their V is zeros too: the tensor map
